@@ -393,6 +393,58 @@ int bp_op_attention_bwd(int dtype, int B, int S, int heads, int head_dim, int ca
                         const float* lse, const void* dctx, void* dqkv, float* delta,
                         void* stream);
 
+/* ---- attention over packed sequences
+ *
+ * Sequences of different lengths lie one behind the other in the rows of q, k, v and ctx: sequence s holds rows
+ * starts[s] .. starts[s + 1] - 1 (none if the two are equal), and its tokens attend each other only.  Rows in front of
+ * starts[0] and from starts[sequences] on belong to no sequence: what they hold does not matter, and results leave them alone.
+ * heads / kv_heads query heads in a row share a key / value head: query head h reads key / value head
+ * h / (heads / kv_heads).
+ *     z[i][j] = scale q[i] . k[j] (+ table[bucket(j - i)][head])        j in i's sequence, causal: j <= i
+ *     lse[i] = log sum_j exp z[i][j]          ctx[i] = sum_j exp(z[i][j] - lse[i]) v[j]
+ * Row t, head h, element c of a tensor lies at t * ld + h * head_dim + c; gradients lie as the tensors they belong to
+ * (dq as q, dk as k, dv as v, dctx as ctx).  bf16 products take the probabilities and the score gradients rounded to
+ * bf16; sums and softmax are fp32. */
+typedef struct {
+    int tokens;             /* rows of every tensor, below 2^24                                      */
+    int sequences;          /* >= 1                                                                  */
+    const int32_t* starts;  /* dev [sequences + 1], ascending, within 0 .. tokens                    */
+    int heads, kv_heads;    /* heads a multiple of kv_heads                                          */
+    int head_dim;           /* 1 .. 512; matrix-core kernels: multiples of 8 up to 128, rows and     */
+                            /* pointers aligned to 16 bytes                                          */
+    int causal;
+    float scale;            /* > 0, or 0: 1 / sqrt(head_dim)                                         */
+    int ld_q, ld_k, ld_v, ld_ctx;   /* elements from one row to the next; 0: heads (kv_heads) * head_dim */
+} bp_packed;
+
+/* Learned relative position bias by buckets.  With causal = 0 half of the buckets hold the offsets j - i > 0, half the
+ * others; with causal all of them hold j - i <= 0.  Of the n buckets of a direction the first e = n / 2 hold one distance
+ * each, 0 .. e - 1; bucket e + m begins at distance e (max_distance / e)^(m / (n - e)); the last one holds all that is farther. */
+typedef struct {
+    int buckets;            /* causal: 2 .. 128; else even, 4 .. 128                                 */
+    int max_distance;       /* above e, below 2^24                                                   */
+    const float* table;     /* dev fp32 [buckets, heads]                                             */
+} bp_relpos;
+
+/* Bucket of offset = key position - query position (pure CPU); BP_EINVAL for what the fields above do not allow. */
+int bp_relpos_bucket(int causal, int buckets, int max_distance, int offset);
+
+/* lse: dev fp32 [heads, tokens].  bias: NULL or the relative position bias. */
+int bp_op_attention_packed_fwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q,
+                               const void* k, const void* v, void* ctx, float* lse, void* stream);
+
+/* fp32 elements of workspace that bp_op_attention_packed_bwd needs (0: arguments that it refuses). */
+size_t bp_op_attention_packed_workspace(int dtype, const bp_packed* layout, const bp_relpos* bias);
+
+/* dq, dk and dv from dctx and the forward's inputs, ctx and lse.  dtable: dev fp32 [buckets, heads], receives += the
+ * gradient of the bias table, overwrite != 0: = (NULL: not wanted; with bf16 it costs a second look at the keys, since the
+ * rounding of ctx would be felt in it).  workspace: dev fp32; its contents need no clearing, and calls that run at the same
+ * time need one each.  The result does not depend on anything but the arguments: no atomic adds across blocks. */
+int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q,
+                               const void* k, const void* v, const void* ctx, const float* lse, const void* dctx,
+                               void* dq, void* dk, void* dv, float* dtable, int overwrite, float* workspace,
+                               size_t workspace_elems, void* stream);
+
 /* Message of the last failure on this thread ("" if none). */
 const char* bp_last_error(void);
 

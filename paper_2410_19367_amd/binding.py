@@ -32,7 +32,8 @@ EXPORTS = (
     "bp_prof_get", "bp_prof_gemm_shapes", "bp_prof_gemm_get", "bp_op_gemm", "bp_op_wgrad_group", "bp_op_layernorm_fwd", "bp_op_layernorm_bwd",
     "bp_op_layernorm_bwd_static", "bp_static_scratch_floats",
     "bp_op_bias_gelu_fwd", "bp_op_bias_gelu_bwd", "bp_op_colsum_workspace",
-    "bp_op_attention_fwd", "bp_op_attention_bwd", "bp_last_error", "bp_version",
+    "bp_op_attention_fwd", "bp_op_attention_bwd", "bp_relpos_bucket", "bp_op_attention_packed_fwd",
+    "bp_op_attention_packed_workspace", "bp_op_attention_packed_bwd", "bp_last_error", "bp_version",
 )
 
 
@@ -49,6 +50,28 @@ class bp_layout(C.Structure):
 class bp_op(C.Structure):
     _fields_ = [("kind", C.c_int8), ("dir", C.c_int8), ("vdev", C.c_int16),
                 ("stage", C.c_int32), ("mb", C.c_int32)]
+
+
+class bp_packed(C.Structure):
+    """Packed sequences.  `starts`: int32 device tensor (kept alive by this object) or its address."""
+    _fields_ = [("tokens", C.c_int), ("sequences", C.c_int), ("starts", C.c_void_p), ("heads", C.c_int),
+                ("kv_heads", C.c_int), ("head_dim", C.c_int), ("causal", C.c_int), ("scale", C.c_float),
+                ("ld_q", C.c_int), ("ld_k", C.c_int), ("ld_v", C.c_int), ("ld_ctx", C.c_int)]
+
+    def __init__(self, tokens, sequences, starts, heads, kv_heads, head_dim, causal, scale=0.0, ld_q=0, ld_k=0, ld_v=0,
+                 ld_ctx=0):
+        super().__init__(tokens, sequences, _ptr(starts), heads, kv_heads, head_dim, int(causal), scale, ld_q, ld_k,
+                         ld_v, ld_ctx)
+        self._starts = starts
+
+
+class bp_relpos(C.Structure):
+    """Relative position bias.  `table`: fp32 device tensor [buckets, heads] (kept alive by this object) or its address."""
+    _fields_ = [("buckets", C.c_int), ("max_distance", C.c_int), ("table", C.c_void_p)]
+
+    def __init__(self, buckets, max_distance, table):
+        super().__init__(buckets, max_distance, _ptr(table))
+        self._table = table
 
 
 class BitPipeError(RuntimeError):
@@ -118,6 +141,13 @@ def lib():
         l.bp_op_colsum_workspace.restype = C.c_size_t
         l.bp_op_attention_fwd.argtypes = [ci, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp]
         l.bp_op_attention_bwd.argtypes = [ci, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp]
+        pp, rp = C.POINTER(bp_packed), C.POINTER(bp_relpos)
+        l.bp_relpos_bucket.argtypes = [ci, ci, ci, ci]
+        l.bp_op_attention_packed_fwd.argtypes = [ci, pp, rp, vp, vp, vp, vp, vp, vp]
+        l.bp_op_attention_packed_workspace.argtypes = [ci, pp, rp]
+        l.bp_op_attention_packed_workspace.restype = C.c_size_t
+        l.bp_op_attention_packed_bwd.argtypes = [ci, pp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp,
+                                                 C.c_size_t, vp]
         l.bp_last_error.restype = C.c_char_p
         l.bp_version.restype = C.c_char_p
         _lib = l
@@ -400,3 +430,28 @@ def bp_op_attention_bwd(dtype, B, S, heads, head_dim, causal, lens, qkv, ctx, ls
     return _check(lib().bp_op_attention_bwd(dtype, B, S, heads, head_dim, int(causal), _ptr(lens),
                                             _ptr(qkv), _ptr(ctx), _ptr(lse), _ptr(dctx), _ptr(dqkv),
                                             _ptr(delta), stream))
+
+
+def bp_relpos_bucket(causal, buckets, max_distance, offset) -> int:
+    b = lib().bp_relpos_bucket(int(causal), buckets, max_distance, offset)
+    if b < 0:
+        _check(b)
+    return b
+
+
+def bp_op_attention_packed_fwd(dtype, layout, q, k, v, ctx, lse, bias=None, stream=None):
+    return _check(lib().bp_op_attention_packed_fwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
+                                                   stream))
+
+
+def bp_op_attention_packed_workspace(dtype, layout, bias=None) -> int:
+    return lib().bp_op_attention_packed_workspace(dtype, layout, bias)
+
+
+def bp_op_attention_packed_bwd(dtype, layout, q, k, v, ctx, lse, dctx, dq, dk, dv, workspace, bias=None, dtable=None,
+                               overwrite=0, workspace_elems=None, stream=None):
+    """workspace_elems: fp32 elements of the workspace (default: those of the tensor)."""
+    n = workspace_elems if workspace_elems is not None else workspace.numel() if workspace is not None else 0
+    return _check(lib().bp_op_attention_packed_bwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
+                                                   _ptr(dctx), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), overwrite,
+                                                   _ptr(workspace), n, stream))

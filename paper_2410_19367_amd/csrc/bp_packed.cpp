@@ -1,0 +1,158 @@
+// C ABI of the attention over packed sequences: argument checks, the borders of the position buckets, and which
+// kernels take a call.
+#include <math.h>
+
+#include "bp_host.h"
+#include "bp_packed.h"
+
+using bp::fail;
+
+namespace bp {
+namespace {
+
+// Whole numbers of up to 256 * 32 bits: x^m e^k with factors below 2^24 and m + k below 256 has fewer.
+struct Wide {
+    uint32_t w[256] = {1};
+    int n = 1;
+    void times(uint32_t f, int count) {
+        for (; count > 0; --count) {
+            uint64_t carry = 0;
+            for (int i = 0; i < n; ++i) {
+                carry += (uint64_t)w[i] * f;
+                w[i] = (uint32_t)carry;
+                carry >>= 32;
+            }
+            if (carry) w[n++] = (uint32_t)carry;
+        }
+    }
+    bool at_least(const Wide& o) const {
+        if (n != o.n) return n > o.n;
+        for (int i = n - 1; i >= 0; --i)
+            if (w[i] != o.w[i]) return w[i] > o.w[i];
+        return true;
+    }
+};
+
+// Smallest whole x with x >= e (far / e)^(k / m).  Where the value in 64 bits is next to a whole number the powers decide,
+// so that a distance on a border belongs to the bucket that begins there.
+int border(int e, int far, int k, int m) {
+    const double y = e * exp(log((double)far / e) * k / m), r = nearbyint(y);
+    if (fabs(y - r) > 1e-11 * y) return (int)ceil(y);
+    Wide a, b;
+    a.times((uint32_t)r, m); a.times((uint32_t)e, k);
+    b.times((uint32_t)far, k); b.times((uint32_t)e, m);
+    return a.at_least(b) ? (int)r : (int)r + 1;
+}
+
+int make_relpos(int causal, int buckets, int max_distance, RelPos& r) {
+    const int n = causal ? buckets : buckets / 2, e = n / 2;
+    if (buckets > kMaxBuckets || n < 2 || (!causal && buckets % 2))
+        return fail(BP_EINVAL, "buckets = %d: with a causal mask 2 .. %d, else even and 4 .. %d", buckets, kMaxBuckets, kMaxBuckets);
+    if (max_distance <= e || max_distance >= 1 << 24)
+        return fail(BP_EINVAL, "max_distance = %d must be above %d (buckets of one distance) and below 2^24", max_distance, e);
+    r.buckets = buckets; r.n = n; r.exact = e;
+    for (int i = 0; i < e; ++i) r.start[i] = i;
+    for (int i = e; i < n; ++i) r.start[i] = border(e, max_distance, i - e, n - e);
+    r.far = r.start[n - 1];
+    r.log2_exact = (float)log2((double)e);
+    r.per_octave = (float)((n - e) / log2((double)max_distance / e));
+    return BP_OK;
+}
+
+int dense(int ld, int heads, int d) { return ld ? ld : heads * d; }
+
+// everything about the layout and the bias; pointers of the tensors are the callers' business
+int make_args(int dtype, const bp_packed* p, const bp_relpos* bias, PackedArgs& a) {
+    if (dtype != BP_F32 && dtype != BP_BF16) return fail(BP_EINVAL, "unknown dtype %d", dtype);
+    if (!p) return fail(BP_EINVAL, "null layout");
+    if (!p->starts) return fail(BP_EINVAL, "null starts");
+    if (p->tokens <= 0 || p->sequences <= 0 || p->heads <= 0 || p->kv_heads <= 0 || p->head_dim <= 0)
+        return fail(BP_EINVAL, "tokens, sequences, heads, kv_heads, head_dim must be positive");
+    if (p->heads % p->kv_heads) return fail(BP_EINVAL, "%d heads cannot share %d key/value heads evenly", p->heads, p->kv_heads);
+    if (!(p->scale >= 0.f) || isinf(p->scale)) return fail(BP_EINVAL, "scale must be positive and finite, or 0");
+    if (p->tokens >= 1 << 24) return fail(BP_ESHAPE, "tokens = %d must be below 2^24", p->tokens);
+    if (p->head_dim > kPackedMaxHeadDim) return fail(BP_ESHAPE, "head_dim = %d must be at most %d", p->head_dim, kPackedMaxHeadDim);
+    if (p->heads > 65535 / 8) return fail(BP_ESHAPE, "heads = %d must be at most %d", p->heads, 65535 / 8);
+    a.T = p->tokens; a.n_seq = p->sequences; a.heads = p->heads; a.kv_heads = p->kv_heads; a.d = p->head_dim;
+    a.causal = p->causal != 0;
+    a.starts = p->starts;
+    a.scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim);
+    a.ld_q = dense(p->ld_q, a.heads, a.d);
+    a.ld_k = dense(p->ld_k, a.kv_heads, a.d);
+    a.ld_v = dense(p->ld_v, a.kv_heads, a.d);
+    a.ld_o = dense(p->ld_ctx, a.heads, a.d);
+    if (a.ld_q < a.heads * a.d || a.ld_o < a.heads * a.d || a.ld_k < a.kv_heads * a.d || a.ld_v < a.kv_heads * a.d)
+        return fail(BP_EINVAL, "leading dimension smaller than the row length");
+    if (a.ld_q >= 1 << 24 || a.ld_k >= 1 << 24 || a.ld_v >= 1 << 24 || a.ld_o >= 1 << 24)
+        return fail(BP_ESHAPE, "leading dimensions must be below 2^24");
+    if (bias) {
+        if (!bias->table) return fail(BP_EINVAL, "null bias table");
+        const int rc = make_relpos(a.causal, bias->buckets, bias->max_distance, a.rel);
+        if (rc) return rc;
+        a.rel.table = bias->table;
+    }
+    return BP_OK;
+}
+
+// floats of the backward's workspace: delta, then the partials of the table's gradient
+size_t delta_floats(const PackedArgs& a) { return ((size_t)a.heads * a.T + 3) & ~(size_t)3; }
+size_t workspace_floats(const PackedArgs& a) {
+    return delta_floats(a) + (size_t)packed_tiles(a.T) * a.heads * a.rel.buckets;
+}
+
+}  // namespace
+}  // namespace bp
+
+extern "C" {
+
+int bp_relpos_bucket(int causal, int buckets, int max_distance, int offset) {
+    bp::RelPos r;
+    const int rc = bp::make_relpos(causal, buckets, max_distance, r);
+    if (rc) return rc;
+    if (causal && offset > 0) return fail(BP_EINVAL, "offset %d: a causal query sees no later key", offset);
+    const int64_t dist = offset < 0 ? -(int64_t)offset : offset;
+    int b = r.n - 1;
+    while (r.start[b] > dist) --b;
+    return b + (offset > 0 ? r.n : 0);
+}
+
+int bp_op_attention_packed_fwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q, const void* k,
+                               const void* v, void* ctx, float* lse, void* stream) {
+    bp::PackedArgs a{};
+    const int rc = bp::make_args(dtype, layout, bias, a);
+    if (rc) return rc;
+    if (!q || !k || !v || !ctx || !lse) return fail(BP_EINVAL, "null pointer");
+    a.q = q; a.k = k; a.v = v; a.ctx = ctx; a.lse = lse;
+    const hipError_t e = bp::launch_packed_fwd_rows(dtype, a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(BP_EHIP, "packed attention forward: %s", hipGetErrorString(e));
+    return BP_OK;
+}
+
+size_t bp_op_attention_packed_workspace(int dtype, const bp_packed* layout, const bp_relpos* bias) {
+    bp::PackedArgs a{};
+    if (bp::make_args(dtype, layout, bias, a)) return 0;
+    return bp::workspace_floats(a);
+}
+
+int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q, const void* k,
+                               const void* v, const void* ctx, const float* lse, const void* dctx, void* dq, void* dk,
+                               void* dv, float* dtable, int overwrite, float* workspace, size_t workspace_elems,
+                               void* stream) {
+    bp::PackedArgs a{};
+    const int rc = bp::make_args(dtype, layout, bias, a);
+    if (rc) return rc;
+    if (!q || !k || !v || !ctx || !lse || !dctx || !dq || !dk || !dv || !workspace) return fail(BP_EINVAL, "null pointer");
+    if (dtable && !bias) return fail(BP_EINVAL, "the gradient of a bias table without a bias");
+    if (workspace_elems < bp::workspace_floats(a))
+        return fail(BP_EINVAL, "workspace of %zu floats, %zu needed", workspace_elems, bp::workspace_floats(a));
+    a.q = q; a.k = k; a.v = v; a.ctx = (void*)ctx; a.lse = (float*)lse;
+    a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv;
+    a.delta = workspace;
+    a.table_part = dtable ? workspace + bp::delta_floats(a) : nullptr;
+    hipError_t e = bp::launch_packed_bwd_rows(dtype, a, (hipStream_t)stream);
+    if (e == hipSuccess && dtable) e = bp::launch_packed_table_grad(a, dtable, overwrite, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(BP_EHIP, "packed attention backward: %s", hipGetErrorString(e));
+    return BP_OK;
+}
+
+}  // extern "C"

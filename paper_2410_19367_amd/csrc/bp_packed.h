@@ -1,0 +1,77 @@
+// Attention over packed sequences: arguments of the launchers, and what every kernel does with them: the rows that a
+// row sees (its sequence, found in the starts) and the bucket of a relative position.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+
+namespace bp {
+
+constexpr int kMaxBuckets = 128;
+constexpr int kPackedMaxHeadDim = 512;
+constexpr int kPackedTile = 64;             // rows that share one partial of the bias table's gradient
+
+// Buckets of a relative position: `first` of the offsets in front of the query (0), behind it (n; bidirectional only),
+// plus the number of starts at or below the distance, minus one.
+struct RelPos {
+    int buckets = 0;                        // all of them; 0: no bias
+    int n = 0;                              // of a direction
+    int exact = 0;                          // buckets of one distance each
+    int far = 0;                            // start[n - 1]: the last bucket has everything from there on
+    float log2_exact = 0.f, per_octave = 0.f;      // bucket ~ exact + (log2(distance) - log2_exact) * per_octave, off by less than one
+    const float* table = nullptr;           // [buckets, heads]
+    int start[kMaxBuckets] = {};
+};
+
+struct PackedArgs {
+    int T, n_seq, heads, kv_heads, d, causal;
+    const int32_t* starts;
+    float scale;
+    int ld_q, ld_k, ld_v, ld_o;
+    const void* q; const void* k; const void* v;
+    void* ctx;
+    float* lse;                             // [heads, T]
+    // backward
+    const void* dctx;
+    void* dq; void* dk; void* dv;
+    float* delta;                           // [heads, T]
+    float* table_part;                      // [tiles of kPackedTile rows][heads][buckets], or null: no gradient of the table
+    RelPos rel;
+};
+
+inline int packed_tiles(int T) { return (T + kPackedTile - 1) / kPackedTile; }
+
+// one row per block, any head width, strides and alignment
+hipError_t launch_packed_fwd_rows(int dtype, const PackedArgs& a, hipStream_t s);
+hipError_t launch_packed_bwd_rows(int dtype, const PackedArgs& a, hipStream_t s);
+// dtable (+)= the partials, in a fixed order
+hipError_t launch_packed_table_grad(const PackedArgs& a, float* dtable, int overwrite, hipStream_t s);
+
+#ifdef __HIPCC__
+// Rows lo .. hi - 1 of the sequence that row t lies in; false: in none.  Whatever the starts hold, the rows named are
+// rows of the tensors.
+__device__ __forceinline__ bool packed_row_range(const PackedArgs& a, int t, int& lo, int& hi) {
+    int s = 0, e = a.n_seq;                 // starts[s] <= t < starts[e], if they do at the ends
+    if (a.starts[0] > t || a.starts[a.n_seq] <= t) return false;
+    while (e - s > 1) {
+        const int m = (s + e) >> 1;
+        if (a.starts[m] <= t) s = m; else e = m;
+    }
+    lo = max(a.starts[s], 0);
+    hi = min(a.starts[e], a.T);
+    return lo <= t && t < hi;
+}
+
+// bucket of an offset (key minus query); with a causal mask only offsets up to 0 occur
+__device__ __forceinline__ int packed_bucket(const RelPos& r, const int* start, int causal, int offset) {
+    const int dist = offset < 0 ? -offset : offset;
+    int s = 0, e = r.n;
+    while (e - s > 1) {
+        const int m = (s + e) >> 1;
+        if (start[m] <= dist) s = m; else e = m;
+    }
+    return s + (!causal && offset > 0 ? r.n : 0);
+}
+#endif
+
+}  // namespace bp
