@@ -15,7 +15,7 @@ SOURCES = [
     "bp_stage.cpp", "bp_schedule.cpp", "bp_ops.cpp", "bp_dispatch.cpp", "bp_packed.cpp",
     "kernels_rowwise.hip", "kernels_generic.hip", "kernels_gemm_mfma.hip", "kernels_gemm_f32.hip",
     "kernels_attn_mfma.hip", "kernels_attn_f32.hip",
-    "kernels_packed_rows.hip", "bp_static_scratch.hip",
+    "kernels_packed_rows.hip", "kernels_packed_bf16.hip", "kernels_packed_f32.hip", "bp_static_scratch.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -94,6 +94,22 @@ int make_args(int dtype, const bp_packed* p, const bp_relpos* bias, PackedArgs& 
     return BP_OK;
 }
 
+// What the kernels on the matrix cores take: heads whose rows are whole 16-byte pieces and fit a tile, and tiles of 64 rows
+// within the 2 GiB that an offset into them may have.
+bool on_matrix_cores(int dtype, const PackedArgs& a) {
+    const int e = dtype == BP_BF16 ? 2 : 4;
+    if (a.d % 8 || a.d > 128) return false;
+    for (int ld : {a.ld_q, a.ld_k, a.ld_v, a.ld_o})
+        if (ld * e % 16 || (int64_t)ld * e * 64 > (int64_t)1 << 31) return false;
+    for (const void* p : {a.q, a.k, a.v, (const void*)a.ctx, a.dctx, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+        if ((uintptr_t)p & 15) return false;
+    return true;
+}
+hipError_t launch(int dtype, const PackedArgs& a, bool back, hipStream_t s) {
+    if (on_matrix_cores(dtype, a)) return dtype == BP_BF16 ? launch_packed_bf16(a, back, s) : launch_packed_f32(a, back, s);
+    return back ? launch_packed_bwd_rows(dtype, a, s) : launch_packed_fwd_rows(dtype, a, s);
+}
+
 // floats of the backward's workspace: delta, then the partials of the table's gradient
 size_t delta_floats(const PackedArgs& a) { return ((size_t)a.heads * a.T + 3) & ~(size_t)3; }
 size_t workspace_floats(const PackedArgs& a) {
@@ -123,7 +139,7 @@ int bp_op_attention_packed_fwd(int dtype, const bp_packed* layout, const bp_relp
     if (rc) return rc;
     if (!q || !k || !v || !ctx || !lse) return fail(BP_EINVAL, "null pointer");
     a.q = q; a.k = k; a.v = v; a.ctx = ctx; a.lse = lse;
-    const hipError_t e = bp::launch_packed_fwd_rows(dtype, a, (hipStream_t)stream);
+    const hipError_t e = bp::launch(dtype, a, false, (hipStream_t)stream);
     if (e != hipSuccess) return fail(BP_EHIP, "packed attention forward: %s", hipGetErrorString(e));
     return BP_OK;
 }
@@ -149,7 +165,7 @@ int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relp
     a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv;
     a.delta = workspace;
     a.table_part = dtable ? workspace + bp::delta_floats(a) : nullptr;
-    hipError_t e = bp::launch_packed_bwd_rows(dtype, a, (hipStream_t)stream);
+    hipError_t e = bp::launch(dtype, a, true, (hipStream_t)stream);
     if (e == hipSuccess && dtable) e = bp::launch_packed_table_grad(a, dtable, overwrite, (hipStream_t)stream);
     if (e != hipSuccess) return fail(BP_EHIP, "packed attention backward: %s", hipGetErrorString(e));
     return BP_OK;

@@ -44,6 +44,9 @@ inline int packed_tiles(int T) { return (T + kPackedTile - 1) / kPackedTile; }
 // one row per block, any head width, strides and alignment
 hipError_t launch_packed_fwd_rows(int dtype, const PackedArgs& a, hipStream_t s);
 hipError_t launch_packed_bwd_rows(int dtype, const PackedArgs& a, hipStream_t s);
+// on the matrix cores: head widths that are multiples of 8 up to 128, 16-byte rows
+hipError_t launch_packed_bf16(const PackedArgs& a, bool back, hipStream_t s);
+hipError_t launch_packed_f32(const PackedArgs& a, bool back, hipStream_t s);
 // dtable (+)= the partials, in a fixed order
 hipError_t launch_packed_table_grad(const PackedArgs& a, float* dtable, int overwrite, hipStream_t s);
 

@@ -1,0 +1,902 @@
+// Attention over packed sequences on the gfx950 matrix cores: forward, dQ, dK / dV, for the element types that supply a
+// policy P (bf16, fp32): tiles of 64 rows in LDS and the products on them.
+//
+// The rows of all sequences are cut into blocks where they lie, wherever the sequences begin: a block may hold the end of
+// one sequence, several whole ones and the start of another, so thousands of short sequences cost no more blocks than one
+// long one.  What a row sees is a range of rows (its sequence, up to itself under a causal mask), and so is what a key is
+// seen by; a block walks the tiles from the first row of its first range to the last of its last, and masks by range only
+// the pieces of 32 x 32 that are not inside every row's range.  Ranges come from the starts: one load of 64 of them and a
+// scalar walk in every wave, no launch before the kernel and nothing on the host.
+//
+// Scores stand transposed where that keeps the softmax row of a query in one lane (forward, dQ: lane <-> query, registers
+// <-> keys; dK/dV: lane <-> key, registers <-> queries), and leave the accumulators as the B operand of the next product.
+//
+// Values that are not finite.  A masked pair has p = 0, but zero times NaN is not zero in the second product.  Only NaN
+// comes of that, so a block that ends with NaN in a result takes its tiles once more, with the second products done row by
+// row on the vector units and the masked pairs left out (some fifteen times the time of the first walk).  A block without
+// NaN pays one look at its results; the second walk is code of its own, without a branch to the matrix cores in it, which
+// kept all accumulators twice (registers of the forward at width 64: 112 alone, 118 with this walk, 162 with the branch).
+//
+// Key / value heads that several query heads share: blocks of query heads of the same one run on the same XCD (position
+// modulo kv_heads first), and a dK/dV block walks its heads one after the other, so shared gradients are sums in
+// registers, in a fixed order.
+#pragma once
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "bp_device.h"
+#include "bp_packed.h"
+#include "bp_tile.h"
+
+namespace bp {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---- what a row sees
+
+// Ranges of the sequences that rows first + lane + 64 r lie in (lo < 0: none), the same rows in every wave of a block.
+// Nothing the starts hold leads outside [0, T).
+template <int R>
+__device__ __forceinline__ void seq_ranges(const int32_t* starts, int n_seq, int T, int first, int lane, int (&lo)[R], int (&hi)[R]) {
+    const int last = first + 64 * R - 1;
+    int base = 0, count = n_seq + 1;
+    while (count > 64) {                    // 64 samples narrow the place of `first` to a 64th
+        const int stride = (count + 63) >> 6, i = lane * stride;
+        const int v = i < count ? starts[base + i] : 0x7fffffff;
+        const int below = max((int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(v <= first)), 1) - 1;
+        base += below * stride;
+        count = min(stride, count - below * stride);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) { lo[r] = -1; hi[r] = 0x7fffffff; }
+    for (int w = base; w <= n_seq; w += 64) {
+        const int v = w + lane <= n_seq ? starts[w + lane] : 0x7fffffff;
+        const int n = min(64, n_seq + 1 - w);
+        int st = 0;
+        for (int e = 0; e < n; ++e) {
+            st = __builtin_amdgcn_readlane(v, e);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int row = first + lane + 64 * r;
+                if (st <= row) { lo[r] = max(st, 0); hi[r] = 0x7fffffff; }
+                else hi[r] = min(hi[r], st);
+            }
+            if (st > last) break;
+        }
+        if (st > last) break;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = first + lane + 64 * r;
+        if (hi[r] == 0x7fffffff || row >= T) lo[r] = -1;
+        hi[r] = min(hi[r], T);
+    }
+}
+
+// The ranges of a lane's row, of the 32 rows of its wave and of all rows of its block.  Ranges of rows that follow one
+// another begin and end in that order, so the outermost and innermost ends are those of the first and last row that has one.
+struct Ranges {
+    int lo, hi;                             // of this lane's row; lo == hi: none
+    int wave_lo, wave_hi, inner_lo, inner_hi;       // outermost and innermost ends of the wave's rows; wave_hi 0: none
+    int blk_lo, blk_hi;                     // outermost ends of the block's; blk_hi 0: none
+};
+// rows: 64 or 128 of a block; mine: this lane's row within it.  by_key: what a key is seen by, else what a query sees
+template <int QB>
+__device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, int mine, int lane, bool by_key) {
+    constexpr int R = QB / 64;
+    int lo[R], hi[R];
+    seq_ranges<R>(a.starts, a.n_seq, a.T, first, lane, lo, hi);
+    Ranges x;
+    x.blk_lo = x.blk_hi = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = first + lane + 64 * r;
+        const bool ok = lo[r] >= 0;
+        if (ok && a.causal) { if (by_key) lo[r] = row; else hi[r] = row + 1; }
+        if (!ok) lo[r] = hi[r] = 0;
+        const uint64_t valid = __builtin_amdgcn_ballot_w64(ok);
+        if (valid) {
+            if (!x.blk_hi) x.blk_lo = __builtin_amdgcn_readlane(lo[r], __builtin_ctzll(valid));
+            x.blk_hi = __builtin_amdgcn_readlane(hi[r], 63 - __builtin_clzll(valid));
+        }
+    }
+    x.lo = __shfl(lo[0], mine & 63, 64);
+    x.hi = __shfl(hi[0], mine & 63, 64);
+    if (R == 2 && mine >= 64) {             // (the same answer in every lane of a wave)
+        x.lo = __shfl(lo[R - 1], mine & 63, 64);
+        x.hi = __shfl(hi[R - 1], mine & 63, 64);
+    }
+    const uint64_t valid = __builtin_amdgcn_ballot_w64(x.hi > x.lo);
+    x.wave_lo = x.wave_hi = x.inner_lo = x.inner_hi = 0;
+    if (valid) {
+        const int f = __builtin_ctzll(valid), l = 63 - __builtin_clzll(valid);
+        const int f_lo = __builtin_amdgcn_readlane(x.lo, f), f_hi = __builtin_amdgcn_readlane(x.hi, f);
+        const int l_lo = __builtin_amdgcn_readlane(x.lo, l), l_hi = __builtin_amdgcn_readlane(x.hi, l);
+        x.wave_lo = f_lo; x.inner_lo = l_lo;
+        x.wave_hi = l_hi; x.inner_hi = f_hi;
+        // (lanes l and l + 32 hold the same row; the last of the first half is the last row)
+    }
+    return x;
+}
+
+// Block `bid` of a launch: blocks of rows from the last on (under a causal mask a sequence's last rows have most to do),
+// all heads of one before the next, heads of the same key / value head a multiple of kv_heads apart.
+__device__ __forceinline__ void packed_coords(const PackedArgs& a, int bid, int nblk, bool last_first, int& blk, int& head, int& kvh) {
+    const int i = bid / a.heads, p = bid - i * a.heads, g = p / a.kv_heads;
+    kvh = p - g * a.kv_heads;
+    head = kvh * (a.heads / a.kv_heads) + g;
+    blk = last_first ? nblk - 1 - i : i;
+}
+
+// ---- pieces of tiles
+
+// Direct copy of rows [first, end) of a tile of 64 rows into LDS; its other rows, and columns at and beyond the head width,
+// become zeros: they lie outside the buffer descriptor's range (up to 2^31 bytes), against which the lane's offset is checked.
+template <class P, int NW>
+struct TileLoader {
+    static constexpr int E = sizeof(typename P::elem), CPR = P::D * E / 16;        // 16-byte chunks per row
+    static constexpr int NI = CPR / NW, ROWSTEP = NW * 64 / CPR;        // rows between a lane's consecutive chunks
+    static constexpr int NO = ROWSTEP >= 16 ? 1 : 16 / ROWSTEP;         // chunks after which the swizzle repeats
+    static constexpr uint32_t kBeyond = 0x80000000u;                    // and so is this plus any row's offset
+    uint32_t off[NO];
+    __device__ __forceinline__ void init(int wave, int lane, int ld, int d) {
+        const int p = wave * 64 + lane;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) {
+            const int row = p / CPR + i * ROWSTEP, c = (p % CPR) ^ P::swizzle(row);
+            off[i] = c * (16 / E) < d ? (uint32_t)(row * ld + c * (16 / E)) * E : kBeyond;
+        }
+    }
+    __device__ __forceinline__ void issue(const typename P::elem* base, int ld, int d, int first, int end, char* lds, int wave) const {
+        const rsrc_t src = make_rsrc(base, (uint32_t)((min(end, 64) - 1) * ld + d) * E);
+        const uint32_t step = (uint32_t)(ROWSTEP * NO * ld) * E;
+        if (first > 0) {
+            const int row = (wave * 64 + (int)__lane_id()) / CPR;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+                dma16(src, row + i * ROWSTEP < first ? kBeyond : off[i % NO] + (i / NO) * step, 0, lds + (wave + NW * i) * 1024);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dma16(src, off[i % NO] + (i / NO) * step, 0, lds + (wave + NW * i) * 1024);
+    }
+};
+
+__device__ __forceinline__ int piece_row(int v, int h) { return 8 * (v >> 2) + 4 * h + (v & 3); }
+
+// out^T += tile[row0 .. row0 + 31]^T x without the pairs outside [lo, hi), the lane's range counted from row0
+template <class P>
+__device__ __forceinline__ void contract_by_rows(const char* tile, int row0, int lane, int lo, int hi, const f32x16& x,
+                                                 f32x16 (&out)[P::DT]) {
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+        int h = lane >> 5;
+        asm volatile("" : "+v"(h));         // nothing that is made of it waits in registers outside the loop
+        const int reg = (r & 3) + 4 * (r >> 3);
+        float mine = x[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) mine = v == reg ? x[v] : mine;
+        const float other = __shfl_xor(mine, 32, 64);
+        const float w = ((r >> 2) & 1) == h ? mine : other;
+        const bool ok = r >= lo && r < hi;
+#pragma unroll
+        for (int t = 0; t < P::DT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 e = P::four(tile, row0 + r, 32 * t + 8 * g + 4 * h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[t][4 * g + i] += ok ? w * e[i] : 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ bool any_nan(const f32x16 (&x)[DT]) {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) bad |= x[t][v] != x[t][v];
+    return bad;
+}
+template <int DT>
+__device__ __forceinline__ void clear(f32x16 (&x)[DT]) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[t][v] = 0.f;
+}
+
+// LDS of one lane's own, added to in the order of the wave's instructions
+__device__ __forceinline__ void lds_add(float* p, float v) {
+    __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+}
+
+// ---- the bias of a piece
+//
+// A piece of 32 x 32 pairs has 63 offsets.  Far from the diagonal they share a bucket, and the bias is one number that
+// joins the softmax's reference point: no work per pair.  Elsewhere a lane takes the bucket of one offset and leaves its
+// value in `slice`, where a pair finds it at a fixed distance from the lane's own place.
+struct RelLds {
+    const int* start;
+    const float* tab;       // [buckets] of the head, in the units of P::expo
+    float* slice;           // [64] of the wave
+};
+__device__ __forceinline__ int fast_bucket(const RelPos& r, const int* start, int causal, int offset) {
+    const int dist = causal ? max(-offset, 0) : abs(offset);        // (offsets above 0 are masked then)
+    const float up = __builtin_amdgcn_logf((float)max(dist, 1)) - r.log2_exact;
+    int b = min(max(r.exact + (int)(up * r.per_octave), 0), r.n - 1);
+    const int s0 = start[b], s1 = start[min(b + 1, r.n - 1)];       // the estimate is off by less than one
+    if (s0 > dist) --b;
+    else if (b + 1 < r.n && s1 <= dist) ++b;
+    if (dist < r.exact) b = dist;
+    return b + (!causal && offset > 0 ? r.n : 0);
+}
+// offset0: that of slice[0]; step: from one place to the next (+1, -1).  Returns whether the piece has more than one
+// bucket; if not, `value` is its bias; `bucket` is the piece's then, else that of the lane's place.
+__device__ __forceinline__ bool bias_of_piece(const RelPos& r, const RelLds& x, int causal, int offset0, int step, int lane,
+                                              float& value, int& bucket) {
+    const int a = offset0, b = offset0 + 62 * step, low = min(a, b), high = max(a, b);
+    if (high <= -r.far || (!causal && low >= r.far)) {
+        bucket = high < 0 ? r.n - 1 : 2 * r.n - 1;
+        value = x.tab[bucket];
+        return false;
+    }
+    bucket = fast_bucket(r, x.start, causal, offset0 + step * min(lane, 62));
+    value = x.tab[bucket];
+    const int b0 = __builtin_amdgcn_readlane(bucket, 0), b1 = __builtin_amdgcn_readlane(bucket, 62);
+    if (b0 == b1) {
+        value = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(value), 0));
+        bucket = b0;
+        return false;
+    }
+    x.slice[lane] = value;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    return true;
+}
+
+// LDS behind the stages: starts of the buckets, the head's values, a slice per wave
+constexpr size_t kRelHead = (size_t)kMaxBuckets * 8;
+template <int NW> constexpr size_t rel_lds() { return kRelHead + NW * 64 * sizeof(float); }
+
+template <class P, int NW>
+__device__ __forceinline__ RelLds rel_init(const PackedArgs& a, char* lds, int head, int wave) {
+    int* start = (int*)lds;
+    float* tab = (float*)(lds + kMaxBuckets * 4);
+    for (int i = threadIdx.x; i < a.rel.n; i += NW * 64) start[i] = a.rel.start[i];
+    for (int i = threadIdx.x; i < a.rel.buckets; i += NW * 64) tab[i] = a.rel.table[(size_t)i * a.heads + head] * P::kUnit;
+    return {start, tab, (float*)(lds + kRelHead) + wave * 64};
+}
+
+// =====================================================================================
+// Forward.  A block of 64 queries: 2 groups of 32 x (2 NT) parts of the keys of a step, NT tiles of 64; every wave keeps
+// its own online softmax and the parts are merged through LDS at the end.  WIDE: 128 queries, a wave takes 32 of them and
+// whole tiles.
+// =====================================================================================
+template <class P, int NT, bool WIDE, bool BIAS>
+__global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_fwd_kernel(PackedArgs a) {
+    typedef typename P::elem elem;
+    constexpr int NW = 4 * NT, NSUB = WIDE ? 1 : 2 * NT, DT = P::DT;
+    constexpr int QB = WIDE ? 128 : 64, NH = WIDE ? 2 : 1;
+    constexpr int TILE = P::TILE, STAGE = NT * 2 * TILE;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qg = wave / NSUB, sub = wave % NSUB, tj = sub >> 1, kh = sub & 1;
+    int blk, head, kvh;
+    packed_coords(a, blockIdx.x, (a.T + QB - 1) / QB, true, blk, head, kvh);
+    const int q_wave = blk * QB + qg * 32, q_lane = q_wave + (lane & 31);
+    const elem* kbase = (const elem*)a.k + kvh * a.d;
+    const elem* vbase = (const elem*)a.v + kvh * a.d;
+    typename P::Rows qf;
+    P::load(qf, (const elem*)a.q + (size_t)min(q_lane, a.T - 1) * a.ld_q + head * a.d, h, a.d);
+    const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
+    if (!x.blk_hi) return;
+    const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0, nsteps = (nt + NT - 1) / NT;
+    const float c = a.scale * P::kUnit;
+    RelLds rel{};
+    if constexpr (BIAS) rel = rel_init<P, NW>(a, smem + 2 * STAGE, head, wave);
+
+    TileLoader<P, NW> lk, lv;
+    lk.init(wave, lane, a.ld_k, a.d);
+    lv.init(wave, lane, a.ld_v, a.d);
+    auto request = [&](int step) {
+        char* st = smem + (step & 1) * STAGE;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int r0 = (t0 + step * NT + j) * 64;
+            if (step * NT + j >= nt) break;
+            lk.issue(kbase + (size_t)r0 * a.ld_k, a.ld_k, a.d, x.blk_lo - r0, x.blk_hi - r0, st + j * 2 * TILE, wave);
+            lv.issue(vbase + (size_t)r0 * a.ld_v, a.ld_v, a.d, x.blk_lo - r0, x.blk_hi - r0, st + j * 2 * TILE + TILE, wave);
+        }
+    };
+
+    f32x16 ot[DT];
+    float m, lsum;
+    auto walk = [&](auto by_rows) __attribute__((always_inline)) {
+        clear<DT>(ot);
+        m = -INFINITY;
+        lsum = 0.f;
+        request(0);
+        for (int t = 0; t < nsteps; ++t) {
+            BP_WAIT_VMCNT(0);
+            __syncthreads();
+            if (t + 1 < nsteps) request(t + 1);
+            const int tile = t * NT + tj, kw = (t0 + tile) * 64 + 32 * kh;
+            if (tile >= nt || kw >= x.wave_hi || kw + 32 * NH <= x.wave_lo) continue;
+            const char* sk = smem + (t & 1) * STAGE + tj * 2 * TILE;
+            const char* sv = sk + TILE;
+            f32x16 s[NH];
+            clear<NH>(s);
+            P::template scores<NH>(sk, 32 * kh, lane, qf, s);
+            float f[NH], o[NH];             // score in the units of expo: f s + o
+#pragma unroll
+            for (int u = 0; u < NH; ++u) {
+                f[u] = c;
+                o[u] = 0.f;
+                if constexpr (BIAS) {
+                    float value;
+                    int bucket;
+                    if (bias_of_piece(a.rel, rel, a.causal, kw + 32 * u - q_wave - 31, 1, lane, value, bucket)) {
+                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) s[u][v] = __builtin_fmaf(s[u][v], c, b[8 * (v >> 2) + (v & 3)]);
+                        f[u] = 1.f;
+                    } else {
+                        o[u] = value;
+                    }
+                }
+            }
+            const bool masked = kw < x.inner_lo || kw + 32 * NH > x.inner_hi;
+            if (masked) {
+                asm volatile("");           // keeps the condition a branch, not a select per pair of every tile
+#pragma unroll
+                for (int u = 0; u < NH; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if ((unsigned)(kw + 32 * u + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) s[u][v] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < NH; ++u) {
+                float w = s[u][0];
+#pragma unroll
+                for (int v = 1; v < 16; ++v) w = fmaxf(w, s[u][v]);
+                mx = fmaxf(mx, BIAS ? __builtin_fmaf(w, f[u], o[u]) : w);
+            }
+            mx = halves_max(mx);
+            if (!BIAS) mx *= c;
+            // the reference point moves only when a score is more than 8 binary orders above it
+            if (__builtin_amdgcn_ballot_w64(mx > m + 8.f * P::kBit) != 0) {
+                const float m_new = fmaxf(m, mx);
+                const float alpha = m == -INFINITY ? 0.f : P::expo(m - m_new);
+                m = m_new;
+                lsum *= alpha;
+#pragma unroll
+                for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) ot[t2][v] *= alpha;
+            }
+            const float m_use = m == -INFINITY ? 0.f : m;       // nothing but -inf so far: no inf - inf
+#pragma unroll
+            for (int u = 0; u < NH; ++u) {
+                const float off = BIAS ? o[u] - m_use : -m_use;
+                float ps = 0.f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float p = P::expo(__builtin_fmaf(s[u][v], f[u], off));
+                    s[u][v] = p;
+                    ps += p;
+                }
+                lsum += ps;
+            }
+#pragma unroll
+            for (int u = 0; u < NH; ++u) {
+                if constexpr (decltype(by_rows)::value)
+                    contract_by_rows<P>(sv, 32 * (kh + u), lane, x.lo - kw - 32 * u, x.hi - kw - 32 * u, s[u], ot);
+                else
+                    P::contract(sv, 32 * (kh + u), lane, s[u], ot);
+            }
+        }
+    };
+    walk(std::false_type{});
+    if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(ot))) walk(std::true_type{});
+
+    // waves 1 .. NSUB - 1 of a query group hand (m, l, O^T) to wave 0 through LDS; a part may have seen nothing
+    float l = halves_sum(lsum), mm = m;
+    if constexpr (!WIDE) {
+        __syncthreads();
+        constexpr int XO = DT * 16 * 64 + 128;
+        float* xo = (float*)smem + (size_t)qg * (NSUB - 1) * XO;
+        if (sub != 0) {
+            float* mine = xo + (size_t)(sub - 1) * XO;
+#pragma unroll
+            for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mine[(t2 * 16 + v) * 64 + lane] = ot[t2][v];
+            mine[DT * 16 * 64 + lane] = m;
+            mine[DT * 16 * 64 + 64 + lane] = l;
+        }
+        __syncthreads();
+        if (sub != 0) return;
+#pragma unroll
+        for (int j = 0; j < NSUB - 1; ++j) mm = fmaxf(mm, xo[(size_t)j * XO + DT * 16 * 64 + lane]);
+        const float use = mm == -INFINITY ? 0.f : mm;
+        const float a0 = P::expo(m - use);
+        l *= a0;
+#pragma unroll
+        for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) ot[t2][v] *= a0;
+#pragma unroll
+        for (int j = 0; j < NSUB - 1; ++j) {
+            const float* other = xo + (size_t)j * XO;
+            const float aj = P::expo(other[DT * 16 * 64 + lane] - use);
+            l += other[DT * 16 * 64 + 64 + lane] * aj;
+#pragma unroll
+            for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) ot[t2][v] += other[(t2 * 16 + v) * 64 + lane] * aj;
+        }
+    }
+    if (x.hi <= x.lo) return;
+    const float inv = 1.f / l;
+    elem* out = (elem*)a.ctx + (size_t)q_lane * a.ld_o + head * a.d;
+#pragma unroll
+    for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = t2 * 32 + 8 * g + 4 * h;
+            if (col < a.d) P::store(out + col, f32x4{ot[t2][4 * g] * inv, ot[t2][4 * g + 1] * inv, ot[t2][4 * g + 2] * inv, ot[t2][4 * g + 3] * inv});
+        }
+    if (h == 0) a.lse[(size_t)head * a.T + q_lane] = mm * P::kToNatural + log2f(l) * 0.6931471805599453f;
+}
+
+// =====================================================================================
+// dQ, and delta for dK/dV.  Decomposed as the forward:
+//   S^T = K Q^T, P^T = exp(S^T - lse), dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T
+// delta = dO . ctx; where the table's gradient is wanted and ctx is rounded to bf16 it is the sum of P dP over a first
+// walk of the keys instead: the last buckets' sums are small differences of many pairs, and half a percent of them came
+// from the rounding (T 2048).
+//
+// The table's gradient: a piece of one bucket adds dS to a register; in others a lane adds its 16 values into 2 x 64 sums
+// by offset (halves apart, so that no two lanes of an instruction share an address and the order is fixed), and a
+// segmented sum over the 63 places leaves one value for each bucket, added to the wave's own row of sums.
+// =====================================================================================
+template <int NW> constexpr size_t table_lds() { return (size_t)NW * (128 + kMaxBuckets) * sizeof(float); }
+
+template <class P, bool WIDE, bool BIAS>
+__global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dq_kernel(PackedArgs a) {
+    typedef typename P::elem elem;
+    constexpr int NW = 4, DT = P::DT, QB = WIDE ? 128 : 64, TILE = P::TILE, STAGE = 2 * TILE;
+    constexpr int NH = WIDE ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qg = WIDE ? wave : wave >> 1, kh0 = WIDE ? 0 : wave & 1;
+    int blk, head, kvh;
+    packed_coords(a, blockIdx.x, (a.T + QB - 1) / QB, true, blk, head, kvh);
+    const int q_wave = blk * QB + qg * 32, q_lane = q_wave + (lane & 31), q_src = min(q_lane, a.T - 1);
+    const elem* kbase = (const elem*)a.k + kvh * a.d;
+    const elem* vbase = (const elem*)a.v + kvh * a.d;
+    typename P::Rows qf, dof;
+    P::load(qf, (const elem*)a.q + (size_t)q_src * a.ld_q + head * a.d, h, a.d);
+    P::load(dof, (const elem*)a.dctx + (size_t)q_src * a.ld_o + head * a.d, h, a.d);
+    const size_t li = (size_t)head * a.T + q_src;
+    float lse = a.lse[li] * P::kUnit, delta;
+    {
+        typename P::Rows of;
+        P::load(of, (const elem*)a.ctx + (size_t)q_src * a.ld_o + head * a.d, h, a.d);
+        delta = halves_sum(P::dot(of, dof));
+    }
+    const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
+    const bool grad = BIAS && a.table_part;
+    if (!x.blk_hi) {
+        if (grad && threadIdx.x < a.rel.buckets)
+            for (int i = 0; i < QB / 64 && blk * (QB / 64) + i < (a.T + 63) / 64; ++i)
+                a.table_part[((size_t)(blk * (QB / 64) + i) * a.heads + head) * a.rel.buckets + threadIdx.x] = 0.f;
+        return;
+    }
+    const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
+    const float c = a.scale * P::kUnit;
+    RelLds rel{};
+    float* diag = nullptr;      // [2][64] sums by offset of a piece
+    float* sums = nullptr;      // [buckets] of the wave
+    if constexpr (BIAS) {
+        if (x.hi <= x.lo) {     // a row of no sequence, whatever it holds, adds nothing to the table's gradient
+            P::zero(qf);
+            P::zero(dof);
+            delta = 0.f;
+            lse = INFINITY;
+        }
+        rel = rel_init<P, NW>(a, smem + 2 * STAGE, head, wave);
+        float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW>());
+        diag = tg + wave * 128;
+        sums = tg + NW * 128 + wave * kMaxBuckets;
+    }
+    TileLoader<P, NW> lk, lv;
+    lk.init(wave, lane, a.ld_k, a.d);
+    lv.init(wave, lane, a.ld_v, a.d);
+    auto request = [&](int t) {
+        char* st = smem + (t & 1) * STAGE;
+        const int r0 = (t0 + t) * 64;
+        lk.issue(kbase + (size_t)r0 * a.ld_k, a.ld_k, a.d, x.blk_lo - r0, x.blk_hi - r0, st, wave);
+        lv.issue(vbase + (size_t)r0 * a.ld_v, a.ld_v, a.d, x.blk_lo - r0, x.blk_hi - r0, st + TILE, wave);
+    };
+
+    f32x16 dq[DT];
+    // what a walk over the keys is for: delta; dQ; dQ once more for values that are not finite
+    enum { DELTA, GRAD, BY_ROWS };
+    auto walk_keys = [&](auto what) __attribute__((always_inline)) {
+        constexpr int walk = decltype(what)::value;
+        clear<DT>(dq);
+        float far = 0.f, pdp = 0.f;         // sum of dS in pieces of one bucket; of P dP
+        int far_bucket = -1;
+        auto flush = [&]() {
+            if (far_bucket < 0) return;
+            const float s = wave_sum(far);
+            if (lane == 0) sums[far_bucket] += s;
+            far = 0.f;
+        };
+        if (grad)
+            for (int i = lane; i < a.rel.buckets; i += 64) sums[i] = 0.f;
+        request(0);
+        for (int t = 0; t < nt; ++t) {
+            BP_WAIT_VMCNT(0);
+            __syncthreads();
+            if (t + 1 < nt) request(t + 1);
+            const char* sk = smem + (t & 1) * STAGE;
+            const char* sv = sk + TILE;
+#pragma unroll
+            for (int kh = kh0; kh < kh0 + NH; ++kh) {
+                const int kw = (t0 + t) * 64 + 32 * kh;
+                if (kw >= x.wave_hi || kw + 32 <= x.wave_lo) continue;
+                f32x16 s, dp;
+                const float d0 = walk == DELTA ? 0.f : -delta;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = d0; }
+                P::scores2(sk, sv, 32 * kh, lane, qf, dof, s, dp);
+                float f = c, o = -lse;
+                bool mixed = false;
+                int bucket = 0;
+                if constexpr (BIAS) {
+                    float value;
+                    mixed = bias_of_piece(a.rel, rel, a.causal, kw - q_wave - 31, 1, lane, value, bucket);
+                    if (mixed) {
+                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[8 * (v >> 2) + (v & 3)]);
+                        f = 1.f;
+                    } else {
+                        o = value - lse;
+                    }
+                }
+                const bool masked = kw < x.inner_lo || kw + 32 > x.inner_hi;
+                if (masked) {
+                    asm volatile("");
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if ((unsigned)(kw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {
+                            s[v] = -INFINITY;
+                            if (walk != GRAD) dp[v] = 0.f;      // (NaN otherwise, which brings about the last walk)
+                        }
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) dp[v] *= P::expo(__builtin_fmaf(s[v], f, o));      // dS^T, or P dP
+                if constexpr (walk == DELTA) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) pdp += dp[v];
+                    continue;
+                }
+                if constexpr (BIAS) {
+                    if (grad && !mixed) {
+                        bucket = __builtin_amdgcn_readfirstlane(bucket);
+                        if (bucket != far_bucket) flush();
+                        far_bucket = bucket;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) far += dp[v];
+                    } else if (grad) {
+                        diag[lane] = 0.f;
+                        diag[64 + lane] = 0.f;
+                        float* mine = diag + 64 * h + 31 + 4 * h - (lane & 31);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) lds_add(mine + 8 * (v >> 2) + (v & 3), dp[v]);
+                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                        float sum = diag[lane] + diag[64 + lane];
+                        // places of one bucket are neighbours: their first lane ends up with the sum of them all
+                        const int before = __shfl_up(bucket, 1, 64);
+#pragma unroll
+                        for (int k = 1; k < 64; k <<= 1) {
+                            const float next = __shfl_down(sum, k, 64);
+                            const int other = __shfl_down(bucket, k, 64);
+                            if (lane + k < 64 && other == bucket) sum += next;
+                        }
+                        if (lane == 0 || before != bucket) sums[bucket] += sum;
+                    }
+                }
+                if constexpr (walk == BY_ROWS) contract_by_rows<P>(sk, 32 * kh, lane, x.lo - kw, x.hi - kw, dp, dq);
+                else P::contract(sk, 32 * kh, lane, dp, dq);
+            }
+        }
+        if constexpr (walk == DELTA) {
+            delta = halves_sum(pdp);
+            if constexpr (!WIDE) {          // two waves have half the keys of a row each
+                float* ex = (float*)(smem + 2 * STAGE + rel_lds<NW>());         // the place of `diag`
+                ex[wave * 64 + lane] = delta;
+                __syncthreads();
+                delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
+            }
+            __syncthreads();                // (and the stages are free for the next walk)
+        } else if (grad) {
+            flush();
+        }
+    };
+    if constexpr (BIAS && P::kRounds)
+        if (grad) walk_keys(std::integral_constant<int, DELTA>{});
+    walk_keys(std::integral_constant<int, GRAD>{});
+    if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(dq))) walk_keys(std::integral_constant<int, BY_ROWS>{});
+    if (kh0 == 0 && h == 0 && x.hi > x.lo) a.delta[li] = delta;
+
+    __syncthreads();
+    if (grad && threadIdx.x < a.rel.buckets) {
+        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW>()) + NW * 128 + threadIdx.x;
+        // a block of 128 rows has two partials' places
+        float part[2];
+        part[0] = WIDE ? tg[0] + tg[kMaxBuckets] : tg[0] + tg[kMaxBuckets] + tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
+        part[1] = tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
+#pragma unroll
+        for (int i = 0; i < QB / 64; ++i)
+            if (blk * (QB / 64) + i < (a.T + 63) / 64)
+                a.table_part[((size_t)(blk * (QB / 64) + i) * a.heads + head) * a.rel.buckets + threadIdx.x] = part[i];
+    }
+    float* xo = (float*)smem + (WIDE ? 0 : qg * (DT * 16 * 64));
+    if constexpr (!WIDE) {
+        if (kh0 == 1) {
+#pragma unroll
+            for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) xo[(t2 * 16 + v) * 64 + lane] = dq[t2][v];
+        }
+        __syncthreads();
+        if (kh0 == 1) return;
+    }
+    if (x.hi <= x.lo) return;
+    elem* out = (elem*)a.dq + (size_t)q_lane * a.ld_q + head * a.d;
+#pragma unroll
+    for (int t2 = 0; t2 < DT; ++t2)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = (WIDE ? dq[t2][4 * g + e] : dq[t2][4 * g + e] + xo[(t2 * 16 + 4 * g + e) * 64 + lane]) * a.scale;
+            const int col = t2 * 32 + 8 * g + 4 * h;
+            if (col < a.d) P::store(out + col, w);
+        }
+}
+
+// =====================================================================================
+// dK and dV of 64 keys (WIDE: 128) of a key / value head: 2 groups of 32 keys x 2 halves of every tile of 64 queries, the
+// tiles of all heads that share them one after the other.
+//   S = Q K^T, P = exp(S - lse[q]), dP = dO V^T, dS = P (dP - delta[q]), dV^T += dO^T P, dK^T += Q^T dS
+// =====================================================================================
+template <class P, bool WIDE, bool BIAS>
+__global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dkv_kernel(PackedArgs a) {
+    typedef typename P::elem elem;
+    constexpr int NW = 4, DT = P::DT, KB = WIDE ? 128 : 64, TILE = P::TILE;
+    constexpr int NH = WIDE ? 2 : 1;
+    constexpr int STAGE = 2 * TILE + 512 + (BIAS ? kMaxBuckets * 4 : 0);       // Q, dO, -lse[64], -delta[64], the head's values
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = WIDE ? wave : wave >> 1, qh0 = WIDE ? 0 : wave & 1;
+    const int G = a.heads / a.kv_heads;
+    const int blk = blockIdx.x / a.kv_heads, kvh = blockIdx.x - blk * a.kv_heads;       // the first rows have most to do
+    const int k_wave = blk * KB + kg * 32, k_lane = k_wave + (lane & 31), k_src = min(k_lane, a.T - 1);
+    typename P::Rows kf, vf;
+    P::load(kf, (const elem*)a.k + (size_t)k_src * a.ld_k + kvh * a.d, h, a.d);
+    P::load(vf, (const elem*)a.v + (size_t)k_src * a.ld_v + kvh * a.d, h, a.d);
+    const Ranges x = block_ranges<KB>(a, blk * KB, kg * 32 + (lane & 31), lane, true);
+    if (!x.blk_hi) return;
+    const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
+    const float c = a.scale * P::kUnit;
+    RelLds rel{};
+    if constexpr (BIAS) {
+        int* start = (int*)(smem + 2 * STAGE);
+        for (int i = threadIdx.x; i < a.rel.n; i += 256) start[i] = a.rel.start[i];
+        rel = {start, nullptr, (float*)(smem + 2 * STAGE + kMaxBuckets * 4) + wave * 64};
+    }
+    TileLoader<P, NW> lq, lo;
+    lq.init(wave, lane, a.ld_q, a.d);
+    lo.init(wave, lane, a.ld_o, a.d);
+    // Step i takes tile t0 + i % nt of head kvh G + i / nt.  Statistics (waves 0 and 1) and the head's values go through
+    // registers, where they get the sign and the base that the exponential and the accumulators want; they are fetched two
+    // steps ahead, so that nothing waits for them but the wait at the top of a step.
+    const int steps = nt * G;
+    const float* stat = wave == 0 ? a.lse : a.delta;
+    const float stat_factor = wave == 0 ? -P::kUnit : -1.f;
+    auto fetch_stat = [&](int g, int t) {
+        // (rows of the tile that the block's keys are not seen by have those of one that does: what others hold may be NaN)
+        const int row = min(max((t0 + t) * 64 + lane, x.blk_lo), x.blk_hi - 1);
+        return wave < 2 && g < G ? stat[(size_t)(kvh * G + g) * a.T + row] : 0.f;
+    };
+    auto fetch_tab = [&](int g) {
+        return BIAS && g < G && threadIdx.x < a.rel.buckets ? a.rel.table[(size_t)threadIdx.x * a.heads + kvh * G + g] : 0.f;
+    };
+    auto put = [&](float st, float tab, char* stage) {
+        if (wave < 2) ((float*)(stage + 2 * TILE))[wave * 64 + lane] = st * stat_factor;
+        if (BIAS && threadIdx.x < a.rel.buckets) ((float*)(stage + 2 * TILE + 512))[threadIdx.x] = tab * P::kUnit;
+    };
+    auto request = [&](int g, int t, char* stage) {
+        const int r0 = (t0 + t) * 64, col = (kvh * G + g) * a.d;
+        lq.issue((const elem*)a.q + (size_t)r0 * a.ld_q + col, a.ld_q, a.d, x.blk_lo - r0, x.blk_hi - r0, stage, wave);
+        lo.issue((const elem*)a.dctx + (size_t)r0 * a.ld_o + col, a.ld_o, a.d, x.blk_lo - r0, x.blk_hi - r0, stage + TILE, wave);
+    };
+    auto advance = [&](int& g, int& t) { if (++t == nt) { t = 0; ++g; } };
+
+    f32x16 dk[DT], dv[DT];
+    auto walk = [&](auto by_rows) __attribute__((always_inline)) {
+        clear<DT>(dk);
+        clear<DT>(dv);
+        int t = 0, g1 = 0, t1 = 0, g2 = 0, t2 = 0;  // this step's tile; the next step's; the one after it
+        const float st0 = fetch_stat(0, 0), tab0 = fetch_tab(0);
+        advance(g1, t1);
+        float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1);
+        request(0, 0, smem);
+        put(st0, tab0, smem);
+        for (int i = 0; i < steps; ++i) {
+            BP_WAIT_VMCNT(0);
+            __syncthreads();
+            if (i + 1 < steps) {
+                char* next = smem + ((i + 1) & 1) * STAGE;
+                put(st1, tab1, next);
+                request(g1, t1, next);
+                g2 = g1; t2 = t1;
+                advance(g2, t2);
+                st1 = fetch_stat(g2, t2);
+                tab1 = fetch_tab(g2);
+            }
+            const char* sq = smem + (i & 1) * STAGE;
+            const char* sdo = sq + TILE;
+            const int q0 = (t0 + t) * 64;
+            t = t1; g1 = g2; t1 = t2;
+            if constexpr (BIAS) rel.tab = (const float*)(sq + 2 * TILE + 512);
+#pragma unroll
+            for (int qh = qh0; qh < qh0 + NH; ++qh) {
+                const int qw = q0 + 32 * qh;
+                if (qw >= x.wave_hi || qw + 32 <= x.wave_lo) continue;
+                const float* nlse = (const float*)(sq + 2 * TILE) + 32 * qh;
+                const float* ndlt = nlse + 64;
+                f32x16 s, dp;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = ndlt[piece_row(v, h)]; }
+                P::scores2(sq, sdo, 32 * qh, lane, kf, vf, s, dp);
+                float f = c, o = 0.f;
+                if constexpr (BIAS) {
+                    int bucket;
+                    float value;
+                    if (bias_of_piece(a.rel, rel, a.causal, k_wave - qw + 31, -1, lane, value, bucket)) {
+                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[8 * (v >> 2) + (v & 3)]);
+                        f = 1.f;
+                    } else {
+                        o = value;
+                    }
+                }
+                const bool masked = qw < x.inner_lo || qw + 32 > x.inner_hi;
+                if (masked) {
+                    asm volatile("");
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if ((unsigned)(qw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {
+                            s[v] = -INFINITY;
+                            if (decltype(by_rows)::value) dp[v] = 0.f;
+                        }
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    s[v] = P::expo(__builtin_fmaf(s[v], f, BIAS ? nlse[piece_row(v, h)] + o : nlse[piece_row(v, h)]));     // P
+                    dp[v] *= s[v];                                                                                        // dS
+                }
+                if constexpr (decltype(by_rows)::value) {
+                    contract_by_rows<P>(sdo, 32 * qh, lane, x.lo - qw, x.hi - qw, s, dv);
+                    contract_by_rows<P>(sq, 32 * qh, lane, x.lo - qw, x.hi - qw, dp, dk);
+                } else {
+                    P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
+                }
+            }
+        }
+    };
+    walk(std::false_type{});
+    if (__syncthreads_or(x.hi > x.lo && (any_nan<DT>(dk) || any_nan<DT>(dv)))) walk(std::true_type{});
+    float* xo = (float*)smem + (WIDE ? 0 : kg * (2 * DT * 16 * 64));
+    if constexpr (!WIDE) {
+        __syncthreads();
+        if (qh0 == 1) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    xo[(t * 16 + v) * 64 + lane] = dk[t][v];
+                    xo[((DT + t) * 16 + v) * 64 + lane] = dv[t][v];
+                }
+        }
+        __syncthreads();
+        if (qh0 == 1) return;
+    }
+    if (x.hi <= x.lo) return;
+    elem* dk_out = (elem*)a.dk + (size_t)k_lane * a.ld_k + kvh * a.d;
+    elem* dv_out = (elem*)a.dv + (size_t)k_lane * a.ld_v + kvh * a.d;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = t * 32 + 8 * g + 4 * h;
+            f32x4 k4, v4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                k4[e] = (WIDE ? dk[t][4 * g + e] : dk[t][4 * g + e] + xo[(t * 16 + 4 * g + e) * 64 + lane]) * a.scale;
+                v4[e] = WIDE ? dv[t][4 * g + e] : dv[t][4 * g + e] + xo[((DT + t) * 16 + 4 * g + e) * 64 + lane];
+            }
+            if (col >= a.d) continue;
+            P::store(dk_out + col, k4);
+            P::store(dv_out + col, v4);
+        }
+}
+
+// ---- host side
+
+template <typename K>
+static hipError_t allow_lds(K kern, size_t bytes, std::atomic<bool>& set) {
+    if (bytes <= 64 * 1024 || set.load(std::memory_order_acquire)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess) set.store(true, std::memory_order_release);
+    return e;
+}
+
+template <class P, int NT, bool WIDE, bool BIAS>
+static hipError_t launch_fwd(const PackedArgs& a, hipStream_t s) {
+    constexpr int QB = WIDE ? 128 : 64;
+    constexpr size_t stages = (size_t)2 * NT * 2 * P::TILE + (BIAS ? rel_lds<4 * NT>() : 0);
+    constexpr size_t merge = WIDE ? 0 : (size_t)2 * (2 * NT - 1) * (P::DT * 16 * 64 + 128) * sizeof(float);
+    constexpr size_t smem = std::max(stages, merge);
+    static std::atomic<bool> set{false};
+    const hipError_t e = allow_lds(packed_fwd_kernel<P, NT, WIDE, BIAS>, smem, set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((packed_fwd_kernel<P, NT, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * a.heads), dim3(256 * NT), smem, s, a);
+    return hipGetLastError();
+}
+template <class P, bool WIDE, bool BIAS>
+static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
+    constexpr int QB = WIDE ? 128 : 64;
+    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4>() + table_lds<4>() : 0);
+    constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * P::DT * 16 * 64 * sizeof(float));
+    static std::atomic<bool> set{false};
+    const hipError_t e = allow_lds(packed_dq_kernel<P, WIDE, BIAS>, smem, set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((packed_dq_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * a.heads), dim3(256), smem, s, a);
+    return hipGetLastError();
+}
+template <class P, bool WIDE, bool BIAS>
+static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
+    constexpr int KB = WIDE ? 128 : 64;
+    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + 4 * 64 * sizeof(float) : 0);
+    constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
+    static std::atomic<bool> set{false};
+    const hipError_t e = allow_lds(packed_dkv_kernel<P, WIDE, BIAS>, smem, set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((packed_dkv_kernel<P, WIDE, BIAS>), dim3((a.T + KB - 1) / KB * a.kv_heads), dim3(256), smem, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace bp
