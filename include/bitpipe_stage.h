@@ -433,12 +433,14 @@ int bp_relpos_bucket(int causal, int buckets, int max_distance, int offset);
 int bp_op_attention_packed_fwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q,
                                const void* k, const void* v, void* ctx, float* lse, void* stream);
 
-/* fp32 elements of workspace that bp_op_attention_packed_bwd needs (0: arguments that it refuses). */
+/* fp32 elements of workspace for bp_op_attention_packed_bwd (0: arguments that it refuses).  heads * tokens, rounded up to a
+ * multiple of 4, and with a bias as many as (tokens + 63) / 64 * heads * buckets, rounded up likewise, are what it cannot do
+ * without; with less than all, heads that share a key / value head are not spread over the chip where there are few tokens. */
 size_t bp_op_attention_packed_workspace(int dtype, const bp_packed* layout, const bp_relpos* bias);
 
 /* dq, dk and dv from dctx and the forward's inputs, ctx and lse.  dtable: dev fp32 [buckets, heads], receives += the
  * gradient of the bias table, overwrite != 0: = (NULL: not wanted; with bf16 it costs a second look at the keys, since the
- * rounding of ctx would be felt in it).  workspace: dev fp32; its contents need no clearing, and calls that run at the same
+ * rounding of ctx would be felt in it).  workspace: dev fp32, aligned to 16 bytes; its contents need no clearing, and calls that run at the same
  * time need one each.  The result does not depend on anything but the arguments: no atomic adds across blocks. */
 int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q,
                                const void* k, const void* v, const void* ctx, const float* lse, const void* dctx,

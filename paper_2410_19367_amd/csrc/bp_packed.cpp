@@ -110,10 +110,14 @@ hipError_t launch(int dtype, const PackedArgs& a, bool back, hipStream_t s) {
     return back ? launch_packed_bwd_rows(dtype, a, s) : launch_packed_fwd_rows(dtype, a, s);
 }
 
-// floats of the backward's workspace: delta, then the partials of the table's gradient
+// floats of the backward's workspace: delta, the partials of the table's gradient, and sums of dK and dV, which a call can
+// do without
 size_t delta_floats(const PackedArgs& a) { return ((size_t)a.heads * a.T + 3) & ~(size_t)3; }
-size_t workspace_floats(const PackedArgs& a) {
-    return delta_floats(a) + (size_t)packed_tiles(a.T) * a.heads * a.rel.buckets;
+size_t needed_floats(const PackedArgs& a) {
+    return delta_floats(a) + (((size_t)packed_tiles(a.T) * a.heads * a.rel.buckets + 3) & ~(size_t)3);
+}
+size_t part_floats(const PackedArgs& a, int splits) {
+    return splits > 1 ? (size_t)splits * a.T * a.kv_heads * 2 * a.d : 0;
 }
 
 }  // namespace
@@ -147,7 +151,7 @@ int bp_op_attention_packed_fwd(int dtype, const bp_packed* layout, const bp_relp
 size_t bp_op_attention_packed_workspace(int dtype, const bp_packed* layout, const bp_relpos* bias) {
     bp::PackedArgs a{};
     if (bp::make_args(dtype, layout, bias, a)) return 0;
-    return bp::workspace_floats(a);
+    return bp::needed_floats(a) + bp::part_floats(a, bp::split_heads(a, bp::cu_count()));
 }
 
 int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q, const void* k,
@@ -159,12 +163,16 @@ int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relp
     if (rc) return rc;
     if (!q || !k || !v || !ctx || !lse || !dctx || !dq || !dk || !dv || !workspace) return fail(BP_EINVAL, "null pointer");
     if (dtable && !bias) return fail(BP_EINVAL, "the gradient of a bias table without a bias");
-    if (workspace_elems < bp::workspace_floats(a))
-        return fail(BP_EINVAL, "workspace of %zu floats, %zu needed", workspace_elems, bp::workspace_floats(a));
+    if (workspace_elems < bp::needed_floats(a))
+        return fail(BP_EINVAL, "workspace of %zu floats, %zu needed", workspace_elems, bp::needed_floats(a));
+    if ((uintptr_t)workspace & 15) return fail(BP_EINVAL, "workspace must be aligned to 16 bytes");
     a.q = q; a.k = k; a.v = v; a.ctx = (void*)ctx; a.lse = (float*)lse;
     a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv;
     a.delta = workspace;
     a.table_part = dtable ? workspace + bp::delta_floats(a) : nullptr;
+    a.dkv_part = workspace + bp::needed_floats(a);
+    a.splits = bp::split_heads(a, bp::cu_count());
+    if (workspace_elems < bp::needed_floats(a) + bp::part_floats(a, a.splits)) a.splits = 1;
     hipError_t e = bp::launch(dtype, a, true, (hipStream_t)stream);
     if (e == hipSuccess && dtable) e = bp::launch_packed_table_grad(a, dtable, overwrite, (hipStream_t)stream);
     if (e != hipSuccess) return fail(BP_EHIP, "packed attention backward: %s", hipGetErrorString(e));

@@ -36,8 +36,20 @@ struct PackedArgs {
     void* dq; void* dk; void* dv;
     float* delta;                           // [heads, T]
     float* table_part;                      // [tiles of kPackedTile rows][heads][buckets], or null: no gradient of the table
+    int splits;                             // parts of the heads of a key / value head whose dK, dV are summed apart
+    float* dkv_part;                        // splits > 1: [splits][T][kv_heads][dK, dV][d]
     RelPos rel;
 };
+
+// Parts into which the heads that share a key / value head are divided for dK and dV.  One where the blocks of 64 keys fill
+// the chip by themselves: each has G times a dQ block's work, and few of them leave most of the chip idle.
+inline int split_heads(const PackedArgs& a, int cus) {
+    const int G = a.heads / a.kv_heads;
+    const long blocks = (long)((a.T + kPackedTile - 1) / kPackedTile) * a.kv_heads;
+    int s = 1;
+    while (s < G && (G % s || blocks * s < 4L * cus)) ++s;
+    return s;
+}
 
 inline int packed_tiles(int T) { return (T + kPackedTile - 1) / kPackedTile; }
 

@@ -76,9 +76,11 @@ __device__ __forceinline__ void seq_ranges(const int32_t* starts, int n_seq, int
 
 // The ranges of a lane's row, of the 32 rows of its wave and of all rows of its block.  Ranges of rows that follow one
 // another begin and end in that order, so the outermost and innermost ends are those of the first and last row that has one.
+// (A wave takes pieces that none of its rows sees like others, masked: left out by a branch, they made the compiler keep
+// two sets of accumulators.  dK/dV at width 128 spilled 580 bytes a lane, now 136.)
 struct Ranges {
     int lo, hi;                             // of this lane's row; lo == hi: none
-    int wave_lo, wave_hi, inner_lo, inner_hi;       // outermost and innermost ends of the wave's rows; wave_hi 0: none
+    int inner_lo, inner_hi;                 // what all rows of the wave see; inner_hi 0: it has none
     int blk_lo, blk_hi;                     // outermost ends of the block's; blk_hi 0: none
 };
 // rows: 64 or 128 of a block; mine: this lane's row within it.  by_key: what a key is seen by, else what a query sees
@@ -108,13 +110,10 @@ __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, i
         x.hi = __shfl(hi[R - 1], mine & 63, 64);
     }
     const uint64_t valid = __builtin_amdgcn_ballot_w64(x.hi > x.lo);
-    x.wave_lo = x.wave_hi = x.inner_lo = x.inner_hi = 0;
+    x.inner_lo = x.inner_hi = 0;
     if (valid) {
-        const int f = __builtin_ctzll(valid), l = 63 - __builtin_clzll(valid);
-        const int f_lo = __builtin_amdgcn_readlane(x.lo, f), f_hi = __builtin_amdgcn_readlane(x.hi, f);
-        const int l_lo = __builtin_amdgcn_readlane(x.lo, l), l_hi = __builtin_amdgcn_readlane(x.hi, l);
-        x.wave_lo = f_lo; x.inner_lo = l_lo;
-        x.wave_hi = l_hi; x.inner_hi = f_hi;
+        x.inner_lo = __builtin_amdgcn_readlane(x.lo, 63 - __builtin_clzll(valid));
+        x.inner_hi = __builtin_amdgcn_readlane(x.hi, __builtin_ctzll(valid));
         // (lanes l and l + 32 hold the same row; the last of the first half is the last row)
     }
     return x;
@@ -328,7 +327,7 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
             __syncthreads();
             if (t + 1 < nsteps) request(t + 1);
             const int tile = t * NT + tj, kw = (t0 + tile) * 64 + 32 * kh;
-            if (tile >= nt || kw >= x.wave_hi || kw + 32 * NH <= x.wave_lo) continue;
+            if (NT > 1 && tile >= nt) continue;
             const char* sk = smem + (t & 1) * STAGE + tj * 2 * TILE;
             const char* sv = sk + TILE;
             f32x16 s[NH];
@@ -460,14 +459,17 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
 // =====================================================================================
 // dQ, and delta for dK/dV.  Decomposed as the forward:
 //   S^T = K Q^T, P^T = exp(S^T - lse), dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T
-// delta = dO . ctx; where the table's gradient is wanted and ctx is rounded to bf16 it is the sum of P dP over a first
-// walk of the keys instead: the last buckets' sums are small differences of many pairs, and half a percent of them came
-// from the rounding (T 2048).
+// delta = dO . ctx, or the sum of P dP over a first walk of the keys where the rounding of ctx to bf16 would be felt:
+//   the table's gradient is wanted: the last buckets' sums are small differences of many pairs (half a percent of them came
+//     from the rounding at 2048 tokens);
+//   a block has few keys, so that delta is not small beside dP: up to kShort tiles (relative error of dQ over sequences of
+//     1 to 40 tokens 2.8e-3 before, of which 1.7e-3 is the rounding of dQ itself).
 //
 // The table's gradient: a piece of one bucket adds dS to a register; in others a lane adds its 16 values into 2 x 64 sums
 // by offset (halves apart, so that no two lanes of an instruction share an address and the order is fixed), and a
 // segmented sum over the 63 places leaves one value for each bucket, added to the wave's own row of sums.
 // =====================================================================================
+constexpr int kShort = 4;
 template <int NW> constexpr size_t table_lds() { return (size_t)NW * (128 + kMaxBuckets) * sizeof(float); }
 
 template <class P, bool WIDE, bool BIAS>
@@ -556,7 +558,6 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 #pragma unroll
             for (int kh = kh0; kh < kh0 + NH; ++kh) {
                 const int kw = (t0 + t) * 64 + 32 * kh;
-                if (kw >= x.wave_hi || kw + 32 <= x.wave_lo) continue;
                 f32x16 s, dp;
                 const float d0 = walk == DELTA ? 0.f : -delta;
 #pragma unroll
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!WIDE) {          // two waves have half the keys of a row each
-                float* ex = (float*)(smem + 2 * STAGE + rel_lds<NW>());         // the place of `diag`
+                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW>() : 0));         // the place of `diag`
                 ex[wave * 64 + lane] = delta;
                 __syncthreads();
                 delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
@@ -639,8 +640,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             flush();
         }
     };
-    if constexpr (BIAS && P::kRounds)
-        if (grad) walk_keys(std::integral_constant<int, DELTA>{});
+    if constexpr (P::kRounds)
+        if (grad || nt <= kShort) walk_keys(std::integral_constant<int, DELTA>{});
     walk_keys(std::integral_constant<int, GRAD>{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(dq))) walk_keys(std::integral_constant<int, BY_ROWS>{});
     if (kh0 == 0 && h == 0 && x.hi > x.lo) a.delta[li] = delta;
@@ -685,7 +686,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 
 // =====================================================================================
 // dK and dV of 64 keys (WIDE: 128) of a key / value head: 2 groups of 32 keys x 2 halves of every tile of 64 queries, the
-// tiles of all heads that share them one after the other.
+// tiles of the heads that share them one after the other: all of them, or with a.splits > 1 an equal part, whose fp32 sums
+// go to the workspace and are joined in a fixed order by packed_join_kernel (split_heads).
 //   S = Q K^T, P = exp(S - lse[q]), dP = dO V^T, dS = P (dP - delta[q]), dV^T += dO^T P, dK^T += Q^T dS
 // =====================================================================================
 template <class P, bool WIDE, bool BIAS>
@@ -699,8 +701,10 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kg = WIDE ? wave : wave >> 1, qh0 = WIDE ? 0 : wave & 1;
-    const int G = a.heads / a.kv_heads;
-    const int blk = blockIdx.x / a.kv_heads, kvh = blockIdx.x - blk * a.kv_heads;       // the first rows have most to do
+    const int G = a.heads / a.kv_heads / a.splits;                      // heads of this block
+    const int blk = blockIdx.x / (a.kv_heads * a.splits);               // the first rows have most to do
+    const int part = (blockIdx.x - blk * a.kv_heads * a.splits) / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+    const int head0 = kvh * (a.heads / a.kv_heads) + part * G;
     const int k_wave = blk * KB + kg * 32, k_lane = k_wave + (lane & 31), k_src = min(k_lane, a.T - 1);
     typename P::Rows kf, vf;
     P::load(kf, (const elem*)a.k + (size_t)k_src * a.ld_k + kvh * a.d, h, a.d);
@@ -718,7 +722,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     TileLoader<P, NW> lq, lo;
     lq.init(wave, lane, a.ld_q, a.d);
     lo.init(wave, lane, a.ld_o, a.d);
-    // Step i takes tile t0 + i % nt of head kvh G + i / nt.  Statistics (waves 0 and 1) and the head's values go through
+    // Step i takes tile t0 + i % nt of head head0 + i / nt.  Statistics (waves 0 and 1) and the head's values go through
     // registers, where they get the sign and the base that the exponential and the accumulators want; they are fetched two
     // steps ahead, so that nothing waits for them but the wait at the top of a step.
     const int steps = nt * G;
@@ -727,17 +731,17 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     auto fetch_stat = [&](int g, int t) {
         // (rows of the tile that the block's keys are not seen by have those of one that does: what others hold may be NaN)
         const int row = min(max((t0 + t) * 64 + lane, x.blk_lo), x.blk_hi - 1);
-        return wave < 2 && g < G ? stat[(size_t)(kvh * G + g) * a.T + row] : 0.f;
+        return wave < 2 && g < G ? stat[(size_t)(head0 + g) * a.T + row] : 0.f;
     };
     auto fetch_tab = [&](int g) {
-        return BIAS && g < G && threadIdx.x < a.rel.buckets ? a.rel.table[(size_t)threadIdx.x * a.heads + kvh * G + g] : 0.f;
+        return BIAS && g < G && threadIdx.x < a.rel.buckets ? a.rel.table[(size_t)threadIdx.x * a.heads + head0 + g] : 0.f;
     };
     auto put = [&](float st, float tab, char* stage) {
         if (wave < 2) ((float*)(stage + 2 * TILE))[wave * 64 + lane] = st * stat_factor;
         if (BIAS && threadIdx.x < a.rel.buckets) ((float*)(stage + 2 * TILE + 512))[threadIdx.x] = tab * P::kUnit;
     };
     auto request = [&](int g, int t, char* stage) {
-        const int r0 = (t0 + t) * 64, col = (kvh * G + g) * a.d;
+        const int r0 = (t0 + t) * 64, col = (head0 + g) * a.d;
         lq.issue((const elem*)a.q + (size_t)r0 * a.ld_q + col, a.ld_q, a.d, x.blk_lo - r0, x.blk_hi - r0, stage, wave);
         lo.issue((const elem*)a.dctx + (size_t)r0 * a.ld_o + col, a.ld_o, a.d, x.blk_lo - r0, x.blk_hi - r0, stage + TILE, wave);
     };
@@ -773,7 +777,6 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 #pragma unroll
             for (int qh = qh0; qh < qh0 + NH; ++qh) {
                 const int qw = q0 + 32 * qh;
-                if (qw >= x.wave_hi || qw + 32 <= x.wave_lo) continue;
                 const float* nlse = (const float*)(sq + 2 * TILE) + 32 * qh;
                 const float* ndlt = nlse + 64;
                 f32x16 s, dp;
@@ -837,6 +840,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     if (x.hi <= x.lo) return;
     elem* dk_out = (elem*)a.dk + (size_t)k_lane * a.ld_k + kvh * a.d;
     elem* dv_out = (elem*)a.dv + (size_t)k_lane * a.ld_v + kvh * a.d;
+    float* sums = a.splits > 1 ? a.dkv_part + (((size_t)part * a.T + k_lane) * a.kv_heads + kvh) * 2 * a.d : nullptr;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -849,9 +853,27 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 v4[e] = WIDE ? dv[t][4 * g + e] : dv[t][4 * g + e] + xo[((DT + t) * 16 + 4 * g + e) * 64 + lane];
             }
             if (col >= a.d) continue;
-            P::store(dk_out + col, k4);
-            P::store(dv_out + col, v4);
+            if (sums) {
+                *reinterpret_cast<f32x4*>(sums + col) = k4;
+                *reinterpret_cast<f32x4*>(sums + a.d + col) = v4;
+            } else {
+                P::store(dk_out + col, k4);
+                P::store(dv_out + col, v4);
+            }
         }
+}
+
+// dK and dV from the parts' sums, four columns of a row to a thread
+template <class P>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
+    const int per = a.kv_heads * 2 * a.d / 4;           // threads a row
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(i / per), c = (int)(i - (size_t)row * per) * 4, kvh = c / (2 * a.d), col = c - kvh * 2 * a.d;
+    if (row >= min(a.starts[a.n_seq], a.T) || row < a.starts[0]) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.splits; ++p) s += *reinterpret_cast<const f32x4*>(a.dkv_part + ((size_t)p * a.T + row) * a.kv_heads * 2 * a.d + c);
+    if (col < a.d) P::store((typename P::elem*)a.dk + (size_t)row * a.ld_k + kvh * a.d + col, s);
+    else P::store((typename P::elem*)a.dv + (size_t)row * a.ld_v + kvh * a.d + col - a.d, s);
 }
 
 // ---- host side
@@ -879,7 +901,7 @@ static hipError_t launch_fwd(const PackedArgs& a, hipStream_t s) {
 template <class P, bool WIDE, bool BIAS>
 static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
     constexpr int QB = WIDE ? 128 : 64;
-    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4>() + table_lds<4>() : 0);
+    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4>() + table_lds<4>() : 4 * 64 * sizeof(float));
     constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * P::DT * 16 * 64 * sizeof(float));
     static std::atomic<bool> set{false};
     const hipError_t e = allow_lds(packed_dq_kernel<P, WIDE, BIAS>, smem, set);
@@ -895,7 +917,11 @@ static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
     static std::atomic<bool> set{false};
     const hipError_t e = allow_lds(packed_dkv_kernel<P, WIDE, BIAS>, smem, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_dkv_kernel<P, WIDE, BIAS>), dim3((a.T + KB - 1) / KB * a.kv_heads), dim3(256), smem, s, a);
+    hipLaunchKernelGGL((packed_dkv_kernel<P, WIDE, BIAS>), dim3((a.T + KB - 1) / KB * a.kv_heads * a.splits), dim3(256), smem, s, a);
+    if (a.splits > 1) {
+        const size_t threads = (size_t)a.T * (a.kv_heads * 2 * a.d / 4);
+        hipLaunchKernelGGL((packed_join_kernel<P>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    }
     return hipGetLastError();
 }
 

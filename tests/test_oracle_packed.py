@@ -92,9 +92,10 @@ def test_buckets_refused(causal, buckets, far, offset):
 GOOD = dict(tokens=100, sequences=3, starts=4096, heads=8, kv_heads=2, head_dim=64, causal=True)
 
 
-def _calls(layout, bias=None, dtype=bp.BP_BF16, missing=None, workspace_elems=1 << 30, dtable=None):
+def _calls(layout, bias=None, dtype=bp.BP_BF16, missing=None, workspace_elems=1 << 30, dtable=None, workspace_at=4096):
     """Both directions with addresses that nothing may touch before the arguments are refused."""
     a = {n: 4096 for n in ("q", "k", "v", "ctx", "lse", "dctx", "dq", "dk", "dv", "workspace")}
+    a["workspace"] = workspace_at
     if missing:
         a[missing] = None
     yield lambda: bp.bp_op_attention_packed_fwd(dtype, layout, a["q"], a["k"], a["v"], a["ctx"], a["lse"], bias=bias)
@@ -131,10 +132,11 @@ def test_pointers_types_and_workspace_refused():
                 call()
             assert e.value.code == bp.BP_EINVAL
     bwd = lambda **kw: list(_calls(layout, **kw))[1]               # noqa: E731
-    need = bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout, bias)
-    assert need > bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout) > 0
+    need = 100 * 8 + 2 * 8 * 32
+    assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout, bias) >= need
+    assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout) >= 100 * 8
     for call in [bwd(missing=n) for n in ("dctx", "dq", "dk", "dv", "workspace")] + [
-            bwd(bias=bias, workspace_elems=need - 1), bwd(dtable=4096), *_calls(layout, bp.bp_relpos(32, 128, None)),
+            bwd(bias=bias, workspace_elems=need - 1), bwd(dtable=4096), bwd(workspace_at=4100), *_calls(layout, bp.bp_relpos(32, 128, None)),
             *_calls(layout, bp.bp_relpos(1, 128, 4096)), *_calls(layout, bp.bp_relpos(32, 3, 4096))]:
         with pytest.raises(bp.BitPipeError) as e:
             call()
