@@ -208,19 +208,46 @@ __device__ __forceinline__ void clear(f32x16 (&x)[DT]) {
         for (int v = 0; v < 16; ++v) x[t][v] = 0.f;
 }
 
-// LDS of one lane's own, added to in the order of the wave's instructions
-__device__ __forceinline__ void lds_add(float* p, float v) {
-    __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+// a wave's own LDS: what its lanes have written is there for all of them
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// Sums of a piece along its offsets: lane o < 63 gets the sum over the rows r of what lane r - o + 31 of a half has for row r.
+// Eight rows at a time go to LDS, each moved on by its place, and come back as columns: 16 writes and 32 reads without a
+// bank conflict.  (16 ds_add_f32 at the offsets, some 2.5 cycles a lane each: dQ with the table's gradient, 8 sentences, 16
+// heads of 64, 130 us, now 69; 6 documents, 32 heads of 128, 1160 us, now 670.)  What the writes leave out is zero throughout.
+constexpr int kSkewPitch = 40;              // offsets 0 .. 38 of eight rows, and a column of zeros
+__device__ __forceinline__ float sum_by_offset(float* skew, const f32x16& x, int lane) {
+    const int h = lane >> 5;
+    float* put = skew + 4 * h * (kSkewPitch + 1) + 31 - (lane & 31);
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        wave_sync();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put[e * (kSkewPitch + 1)] = x[4 * g + e];
+        wave_sync();
+        const float* get = skew + ((unsigned)(lane - 8 * g) < 39u ? lane - 8 * g : 39);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sum += get[r * kSkewPitch];
+    }
+    return sum;
 }
 
 // ---- the bias of a piece
 //
 // A piece of 32 x 32 pairs has 63 offsets.  Far from the diagonal they share a bucket, and the bias is one number that
-// joins the softmax's reference point: no work per pair.  Elsewhere a lane takes the bucket of one offset and leaves its
-// value in `slice`, where a pair finds it at a fixed distance from the lane's own place.
+// joins the softmax's reference point: no work per pair.  Around the diagonal, where buckets are narrow, the values of
+// kWindow offsets lie in LDS for the whole launch, and a pair reads the one at a fixed distance from its lane's place.
+// A piece outside this window that a border of buckets crosses gets its values by a look-up, a lane for each offset.
+constexpr int kWindow = 256;
+__device__ __forceinline__ int window_base(int causal) { return causal ? kWindow - 32 : kWindow / 2; }     // place of offset 0
 struct RelLds {
-    const int* start;
+    const int* start;       // of the buckets
     const float* tab;       // [buckets] of the head, in the units of P::expo
+    const float* win;       // [kWindow] by offset
     float* slice;           // [64] of the wave
 };
 __device__ __forceinline__ int fast_bucket(const RelPos& r, const int* start, int causal, int offset) {
@@ -233,42 +260,62 @@ __device__ __forceinline__ int fast_bucket(const RelPos& r, const int* start, in
     if (dist < r.exact) b = dist;
     return b + (!causal && offset > 0 ? r.n : 0);
 }
-// offset0: that of slice[0]; step: from one place to the next (+1, -1).  Returns whether the piece has more than one
-// bucket; if not, `value` is its bias; `bucket` is the piece's then, else that of the lane's place.
-__device__ __forceinline__ bool bias_of_piece(const RelPos& r, const RelLds& x, int causal, int offset0, int step, int lane,
-                                              float& value, int& bucket) {
-    const int a = offset0, b = offset0 + 62 * step, low = min(a, b), high = max(a, b);
-    if (high <= -r.far || (!causal && low >= r.far)) {
-        bucket = high < 0 ? r.n - 1 : 2 * r.n - 1;
-        value = x.tab[bucket];
-        return false;
+enum { ONE_BUCKET, IN_WINDOW, LOOKED_UP };
+// The piece whose offsets are offset0 .. offset0 + 62: ONE_BUCKET: `value` is its bias and `bucket` the bucket; else `by`
+// points at offset0's value, and after LOOKED_UP `bucket` is that of the lane's offset (the last one again in lane 63).
+__device__ __forceinline__ int bias_of_piece(const RelPos& r, const RelLds& x, int causal, int offset0, int lane, float& value,
+                                             int& bucket, const float*& by) {
+    const int place = offset0 + window_base(causal);
+    if ((unsigned)place <= (unsigned)(kWindow - 63)) {
+        by = x.win + place;
+        return IN_WINDOW;
     }
-    bucket = fast_bucket(r, x.start, causal, offset0 + step * min(lane, 62));
+    by = x.slice;
+    if (offset0 + 62 <= -r.far || (!causal && offset0 >= r.far)) {
+        bucket = offset0 < 0 ? r.n - 1 : 2 * r.n - 1;
+        value = x.tab[bucket];
+        return ONE_BUCKET;
+    }
+    bucket = fast_bucket(r, x.start, causal, offset0 + min(lane, 62));
     value = x.tab[bucket];
     const int b0 = __builtin_amdgcn_readlane(bucket, 0), b1 = __builtin_amdgcn_readlane(bucket, 62);
     if (b0 == b1) {
         value = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(value), 0));
         bucket = b0;
-        return false;
+        return ONE_BUCKET;
     }
     x.slice[lane] = value;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    return true;
+    wave_sync();
+    return LOOKED_UP;
 }
 
-// LDS behind the stages: starts of the buckets, the head's values, a slice per wave
-constexpr size_t kRelHead = (size_t)kMaxBuckets * 8;
+// LDS behind the stages: starts of the buckets, the head's values by bucket and by offset, a slice per wave
+constexpr size_t kRelHead = (size_t)kMaxBuckets * 8 + kWindow * 4;
 template <int NW> constexpr size_t rel_lds() { return kRelHead + NW * 64 * sizeof(float); }
 
 template <class P, int NW>
 __device__ __forceinline__ RelLds rel_init(const PackedArgs& a, char* lds, int head, int wave) {
     int* start = (int*)lds;
     float* tab = (float*)(lds + kMaxBuckets * 4);
+    float* win = tab + kMaxBuckets;
     for (int i = threadIdx.x; i < a.rel.n; i += NW * 64) start[i] = a.rel.start[i];
     for (int i = threadIdx.x; i < a.rel.buckets; i += NW * 64) tab[i] = a.rel.table[(size_t)i * a.heads + head] * P::kUnit;
-    return {start, tab, (float*)(lds + kRelHead) + wave * 64};
+    for (int i = threadIdx.x; i < kWindow; i += NW * 64)
+        win[i] = a.rel.table[(size_t)fast_bucket(a.rel, a.rel.start, a.causal, i - window_base(a.causal)) * a.heads + head] * P::kUnit;
+    return {start, tab, win, (float*)(lds + kRelHead) + wave * 64};
+}
+
+// Adds what the lanes have for offsets offset0 + lane (buckets `bucket`) to the wave's sums by bucket.  Offsets of one bucket
+// are neighbours: the first lane of them ends up with their sum.
+__device__ __forceinline__ void add_by_bucket(float* sums, int bucket, float sum, int lane) {
+    const int before = __shfl_up(bucket, 1, 64);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const float next = __shfl_down(sum, k, 64);
+        const int other = __shfl_down(bucket, k, 64);
+        if (lane + k < 64 && other == bucket) sum += next;
+    }
+    if (lane == 0 || before != bucket) sums[bucket] += sum;
 }
 
 // =====================================================================================
@@ -341,8 +388,9 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
                 if constexpr (BIAS) {
                     float value;
                     int bucket;
-                    if (bias_of_piece(a.rel, rel, a.causal, kw + 32 * u - q_wave - 31, 1, lane, value, bucket)) {
-                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+                    const float* b;
+                    if (bias_of_piece(a.rel, rel, a.causal, kw + 32 * u - q_wave - 31, lane, value, bucket, b) != ONE_BUCKET) {
+                        b += 31 + 4 * h - (lane & 31);
 #pragma unroll
                         for (int v = 0; v < 16; ++v) s[u][v] = __builtin_fmaf(s[u][v], c, b[8 * (v >> 2) + (v & 3)]);
                         f[u] = 1.f;
@@ -465,12 +513,11 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
 //   a block has few keys, so that delta is not small beside dP: up to kShort tiles (relative error of dQ over sequences of
 //     1 to 40 tokens 2.8e-3 before, of which 1.7e-3 is the rounding of dQ itself).
 //
-// The table's gradient: a piece of one bucket adds dS to a register; in others a lane adds its 16 values into 2 x 64 sums
-// by offset (halves apart, so that no two lanes of an instruction share an address and the order is fixed), and a
-// segmented sum over the 63 places leaves one value for each bucket, added to the wave's own row of sums.
+// The table's gradient: a piece of one bucket adds dS to a register; others are summed by offset (sum_by_offset).  Sums by
+// offset become sums by bucket with a segmented sum over the lanes: of the window once, at the end; of a piece outside at once.
 // =====================================================================================
 constexpr int kShort = 4;
-template <int NW> constexpr size_t table_lds() { return (size_t)NW * (128 + kMaxBuckets) * sizeof(float); }
+template <int NW> constexpr size_t table_lds() { return (size_t)NW * (8 * kSkewPitch + kMaxBuckets + kWindow) * sizeof(float); }
 
 template <class P, bool WIDE, bool BIAS>
 __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dq_kernel(PackedArgs a) {
@@ -508,8 +555,9 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
     const float c = a.scale * P::kUnit;
     RelLds rel{};
-    float* diag = nullptr;      // [2][64] sums by offset of a piece
-    float* sums = nullptr;      // [buckets] of the wave
+    float* skew = nullptr;      // of the wave: for sum_by_offset
+    float* near = nullptr;      // sums by offset, in the window
+    float* sums = nullptr;      // sums by bucket
     if constexpr (BIAS) {
         if (x.hi <= x.lo) {     // a row of no sequence, whatever it holds, adds nothing to the table's gradient
             P::zero(qf);
@@ -519,8 +567,9 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         }
         rel = rel_init<P, NW>(a, smem + 2 * STAGE, head, wave);
         float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW>());
-        diag = tg + wave * 128;
-        sums = tg + NW * 128 + wave * kMaxBuckets;
+        skew = tg + wave * 8 * kSkewPitch;
+        sums = tg + NW * 8 * kSkewPitch + wave * kMaxBuckets;
+        near = tg + NW * (8 * kSkewPitch + kMaxBuckets) + wave * kWindow;
     }
     TileLoader<P, NW> lk, lv;
     lk.init(wave, lane, a.ld_k, a.d);
@@ -546,8 +595,11 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             if (lane == 0) sums[far_bucket] += s;
             far = 0.f;
         };
-        if (grad)
+        if (grad) {
             for (int i = lane; i < a.rel.buckets; i += 64) sums[i] = 0.f;
+            for (int i = lane; i < kWindow; i += 64) near[i] = 0.f;
+            for (int i = lane; i < 8 * kSkewPitch; i += 64) skew[i] = 0.f;
+        }
         request(0);
         for (int t = 0; t < nt; ++t) {
             BP_WAIT_VMCNT(0);
@@ -564,13 +616,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = d0; }
                 P::scores2(sk, sv, 32 * kh, lane, qf, dof, s, dp);
                 float f = c, o = -lse;
-                bool mixed = false;
-                int bucket = 0;
+                int kind = ONE_BUCKET, bucket = 0;
                 if constexpr (BIAS) {
                     float value;
-                    mixed = bias_of_piece(a.rel, rel, a.causal, kw - q_wave - 31, 1, lane, value, bucket);
-                    if (mixed) {
-                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+                    const float* b;
+                    kind = bias_of_piece(a.rel, rel, a.causal, kw - q_wave - 31, lane, value, bucket, b);
+                    if (kind != ONE_BUCKET) {
+                        b += 31 + 4 * h - (lane & 31);
 #pragma unroll
                         for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[8 * (v >> 2) + (v & 3)]);
                         f = 1.f;
@@ -596,31 +648,16 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                     continue;
                 }
                 if constexpr (BIAS) {
-                    if (grad && !mixed) {
+                    if (grad && kind == ONE_BUCKET) {
                         bucket = __builtin_amdgcn_readfirstlane(bucket);
                         if (bucket != far_bucket) flush();
                         far_bucket = bucket;
 #pragma unroll
                         for (int v = 0; v < 16; ++v) far += dp[v];
                     } else if (grad) {
-                        diag[lane] = 0.f;
-                        diag[64 + lane] = 0.f;
-                        float* mine = diag + 64 * h + 31 + 4 * h - (lane & 31);
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) lds_add(mine + 8 * (v >> 2) + (v & 3), dp[v]);
-                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                        float sum = diag[lane] + diag[64 + lane];
-                        // places of one bucket are neighbours: their first lane ends up with the sum of them all
-                        const int before = __shfl_up(bucket, 1, 64);
-#pragma unroll
-                        for (int k = 1; k < 64; k <<= 1) {
-                            const float next = __shfl_down(sum, k, 64);
-                            const int other = __shfl_down(bucket, k, 64);
-                            if (lane + k < 64 && other == bucket) sum += next;
-                        }
-                        if (lane == 0 || before != bucket) sums[bucket] += sum;
+                        const float sum = sum_by_offset(skew, dp, lane);
+                        if (kind == LOOKED_UP) add_by_bucket(sums, bucket, sum, lane);
+                        else if (lane < 63) near[kw - q_wave - 31 + window_base(a.causal) + lane] += sum;
                     }
                 }
                 if constexpr (walk == BY_ROWS) contract_by_rows<P>(sk, 32 * kh, lane, x.lo - kw, x.hi - kw, dp, dq);
@@ -630,7 +667,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!WIDE) {          // two waves have half the keys of a row each
-                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW>() : 0));         // the place of `diag`
+                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW>() : 0));         // the place of `skew`
                 ex[wave * 64 + lane] = delta;
                 __syncthreads();
                 delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
@@ -638,6 +675,9 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             __syncthreads();                // (and the stages are free for the next walk)
         } else if (grad) {
             flush();
+            wave_sync();
+            for (int i = lane; i < kWindow; i += 64)
+                add_by_bucket(sums, fast_bucket(a.rel, rel.start, a.causal, i - window_base(a.causal)), near[i], lane);
         }
     };
     if constexpr (P::kRounds)
@@ -648,7 +688,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 
     __syncthreads();
     if (grad && threadIdx.x < a.rel.buckets) {
-        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW>()) + NW * 128 + threadIdx.x;
+        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW>()) + NW * 8 * kSkewPitch + threadIdx.x;
         // a block of 128 rows has two partials' places
         float part[2];
         part[0] = WIDE ? tg[0] + tg[kMaxBuckets] : tg[0] + tg[kMaxBuckets] + tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
@@ -714,11 +754,16 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
     const float c = a.scale * P::kUnit;
     RelLds rel{};
+    float* wins = nullptr;                  // values by offset, of the heads of even and of odd steps
     if constexpr (BIAS) {
         int* start = (int*)(smem + 2 * STAGE);
         for (int i = threadIdx.x; i < a.rel.n; i += 256) start[i] = a.rel.start[i];
-        rel = {start, nullptr, (float*)(smem + 2 * STAGE + kMaxBuckets * 4) + wave * 64};
+        wins = (float*)(start + kMaxBuckets);
+        rel = {start, nullptr, nullptr, wins + 2 * kWindow + wave * 64};
     }
+    int my_bucket = 0;                      // of this thread's place in the window
+    if constexpr (BIAS) my_bucket = fast_bucket(a.rel, a.rel.start, a.causal, (int)threadIdx.x - window_base(a.causal));
+    static_assert(kWindow == 256, "a place for every thread");
     TileLoader<P, NW> lq, lo;
     lq.init(wave, lane, a.ld_q, a.d);
     lo.init(wave, lane, a.ld_o, a.d);
@@ -736,9 +781,12 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     auto fetch_tab = [&](int g) {
         return BIAS && g < G && threadIdx.x < a.rel.buckets ? a.rel.table[(size_t)threadIdx.x * a.heads + head0 + g] : 0.f;
     };
-    auto put = [&](float st, float tab, char* stage) {
+    auto fetch_win = [&](int g) { return BIAS && g < G ? a.rel.table[(size_t)my_bucket * a.heads + head0 + g] : 0.f; };
+    auto put = [&](float st, float tab, float win, int step) {
+        char* stage = smem + (step & 1) * STAGE;
         if (wave < 2) ((float*)(stage + 2 * TILE))[wave * 64 + lane] = st * stat_factor;
         if (BIAS && threadIdx.x < a.rel.buckets) ((float*)(stage + 2 * TILE + 512))[threadIdx.x] = tab * P::kUnit;
+        if (BIAS) wins[(step & 1) * kWindow + threadIdx.x] = win * P::kUnit;
     };
     auto request = [&](int g, int t, char* stage) {
         const int r0 = (t0 + t) * 64, col = (head0 + g) * a.d;
@@ -752,28 +800,31 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         clear<DT>(dk);
         clear<DT>(dv);
         int t = 0, g1 = 0, t1 = 0, g2 = 0, t2 = 0;  // this step's tile; the next step's; the one after it
-        const float st0 = fetch_stat(0, 0), tab0 = fetch_tab(0);
+        const float st0 = fetch_stat(0, 0), tab0 = fetch_tab(0), win0 = fetch_win(0);
         advance(g1, t1);
-        float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1);
+        float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1), win1 = fetch_win(g1);
         request(0, 0, smem);
-        put(st0, tab0, smem);
+        put(st0, tab0, win0, 0);
         for (int i = 0; i < steps; ++i) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (i + 1 < steps) {
-                char* next = smem + ((i + 1) & 1) * STAGE;
-                put(st1, tab1, next);
-                request(g1, t1, next);
+                put(st1, tab1, win1, i + 1);
+                request(g1, t1, smem + ((i + 1) & 1) * STAGE);
                 g2 = g1; t2 = t1;
                 advance(g2, t2);
                 st1 = fetch_stat(g2, t2);
                 tab1 = fetch_tab(g2);
+                win1 = fetch_win(g2);
             }
             const char* sq = smem + (i & 1) * STAGE;
             const char* sdo = sq + TILE;
             const int q0 = (t0 + t) * 64;
             t = t1; g1 = g2; t1 = t2;
-            if constexpr (BIAS) rel.tab = (const float*)(sq + 2 * TILE + 512);
+            if constexpr (BIAS) {
+                rel.tab = (const float*)(sq + 2 * TILE + 512);
+                rel.win = wins + (i & 1) * kWindow;
+            }
 #pragma unroll
             for (int qh = qh0; qh < qh0 + NH; ++qh) {
                 const int qw = q0 + 32 * qh;
@@ -787,10 +838,11 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 if constexpr (BIAS) {
                     int bucket;
                     float value;
-                    if (bias_of_piece(a.rel, rel, a.causal, k_wave - qw + 31, -1, lane, value, bucket)) {
-                        const float* b = rel.slice + 31 + 4 * h - (lane & 31);
+                    const float* b;
+                    if (bias_of_piece(a.rel, rel, a.causal, k_wave - qw - 31, lane, value, bucket, b) != ONE_BUCKET) {
+                        b += 31 + (lane & 31) - 4 * h - 27;         // offsets fall with the register's row, 0 .. 27 here
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[8 * (v >> 2) + (v & 3)]);
+                        for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[27 - 8 * (v >> 2) - (v & 3)]);
                         f = 1.f;
                     } else {
                         o = value;
@@ -912,7 +964,7 @@ static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
 template <class P, bool WIDE, bool BIAS>
 static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
     constexpr int KB = WIDE ? 128 : 64;
-    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + 4 * 64 * sizeof(float) : 0);
+    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + (2 * kWindow + 4 * 64) * sizeof(float) : 0);
     constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
     static std::atomic<bool> set{false};
     const hipError_t e = allow_lds(packed_dkv_kernel<P, WIDE, BIAS>, smem, set);
