@@ -7,6 +7,8 @@
 
 namespace bp {
 
+int cu_count();          // compute units of the device
+
 constexpr int kMaxBuckets = 128;
 constexpr int kPackedMaxHeadDim = 512;
 constexpr int kPackedTile = 64;             // rows that share one partial of the bias table's gradient

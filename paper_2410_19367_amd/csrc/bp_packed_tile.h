@@ -77,7 +77,7 @@ __device__ __forceinline__ void seq_ranges(const int32_t* starts, int n_seq, int
 // The ranges of a lane's row, of the 32 rows of its wave and of all rows of its block.  Ranges of rows that follow one
 // another begin and end in that order, so the outermost and innermost ends are those of the first and last row that has one.
 // (A wave takes pieces that none of its rows sees like others, masked: left out by a branch, they made the compiler keep
-// two sets of accumulators.  dK/dV at width 128 spilled 580 bytes a lane, now 136.)
+// two sets of accumulators.  dK/dV at width 128 spilled 580 bytes a lane, then 136, in 256 registers.)
 struct Ranges {
     int lo, hi;                             // of this lane's row; lo == hi: none
     int inner_lo, inner_hi;                 // what all rows of the wave see; inner_hi 0: it has none
@@ -119,13 +119,14 @@ __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, i
     return x;
 }
 
-// Block `bid` of a launch: blocks of rows from the last on (under a causal mask a sequence's last rows have most to do),
-// all heads of one before the next, heads of the same key / value head a multiple of kv_heads apart.
-__device__ __forceinline__ void packed_coords(const PackedArgs& a, int bid, int nblk, bool last_first, int& blk, int& head, int& kvh) {
-    const int i = bid / a.heads, p = bid - i * a.heads, g = p / a.kv_heads;
+// Block `bid` of a launch: blocks of rows from the last on (under a causal mask a sequence's last rows have most to do), all
+// heads of one before the next, heads of the same key / value head a multiple of kv_heads apart.  HP heads share a block.
+template <int HP>
+__device__ __forceinline__ void packed_coords(const PackedArgs& a, int bid, int nblk, int& blk, int& head, int& kvh) {
+    const int per = a.heads / HP, i = bid / per, p = bid - i * per, g = p / a.kv_heads;
     kvh = p - g * a.kv_heads;
-    head = kvh * (a.heads / a.kv_heads) + g;
-    blk = last_first ? nblk - 1 - i : i;
+    head = kvh * (a.heads / a.kv_heads) + g * HP;
+    blk = nblk - 1 - i;
 }
 
 // ---- pieces of tiles
@@ -148,7 +149,7 @@ struct TileLoader {
         }
     }
     __device__ __forceinline__ void issue(const typename P::elem* base, int ld, int d, int first, int end, char* lds, int wave) const {
-        const rsrc_t src = make_rsrc(base, (uint32_t)((min(end, 64) - 1) * ld + d) * E);
+        const rsrc_t src = make_rsrc(base, end > 0 ? (uint32_t)((min(end, 64) - 1) * ld + d) * E : 0u);
         const uint32_t step = (uint32_t)(ROWSTEP * NO * ld) * E;
         if (first > 0) {
             const int row = (wave * 64 + (int)__lane_id()) / CPR;
@@ -289,20 +290,26 @@ __device__ __forceinline__ int bias_of_piece(const RelPos& r, const RelLds& x, i
     return LOOKED_UP;
 }
 
-// LDS behind the stages: starts of the buckets, the head's values by bucket and by offset, a slice per wave
-constexpr size_t kRelHead = (size_t)kMaxBuckets * 8 + kWindow * 4;
-template <int NW> constexpr size_t rel_lds() { return kRelHead + NW * 64 * sizeof(float); }
+// LDS behind the stages: starts of the buckets, values by bucket and by offset of the block's HP heads, a slice per wave
+constexpr int kRelHead = kMaxBuckets + kWindow;
+template <int NW, int HP> constexpr size_t rel_lds() { return (kMaxBuckets + HP * kRelHead + NW * 64) * sizeof(float); }
 
-template <class P, int NW>
-__device__ __forceinline__ RelLds rel_init(const PackedArgs& a, char* lds, int head, int wave) {
+// hw: which of the block's heads is the wave's
+template <class P, int NW, int HP>
+__device__ __forceinline__ RelLds rel_init(const PackedArgs& a, char* lds, int head, int hw, int wave) {
     int* start = (int*)lds;
-    float* tab = (float*)(lds + kMaxBuckets * 4);
-    float* win = tab + kMaxBuckets;
+    float* tab = (float*)lds + kMaxBuckets;
     for (int i = threadIdx.x; i < a.rel.n; i += NW * 64) start[i] = a.rel.start[i];
-    for (int i = threadIdx.x; i < a.rel.buckets; i += NW * 64) tab[i] = a.rel.table[(size_t)i * a.heads + head] * P::kUnit;
-    for (int i = threadIdx.x; i < kWindow; i += NW * 64)
-        win[i] = a.rel.table[(size_t)fast_bucket(a.rel, a.rel.start, a.causal, i - window_base(a.causal)) * a.heads + head] * P::kUnit;
-    return {start, tab, win, (float*)(lds + kRelHead) + wave * 64};
+#pragma unroll
+    for (int u = 0; u < HP; ++u) {
+        for (int i = threadIdx.x; i < a.rel.buckets; i += NW * 64)
+            tab[u * kRelHead + i] = a.rel.table[(size_t)i * a.heads + head + u] * P::kUnit;
+        for (int i = threadIdx.x; i < kWindow; i += NW * 64)
+            tab[u * kRelHead + kMaxBuckets + i] =
+                a.rel.table[(size_t)fast_bucket(a.rel, a.rel.start, a.causal, i - window_base(a.causal)) * a.heads + head + u] * P::kUnit;
+    }
+    tab += hw * kRelHead;
+    return {start, tab, tab + kMaxBuckets, (float*)lds + kMaxBuckets + HP * kRelHead + wave * 64};
 }
 
 // Adds what the lanes have for offsets offset0 + lane (buckets `bucket`) to the wave's sums by bucket.  Offsets of one bucket
@@ -319,23 +326,24 @@ __device__ __forceinline__ void add_by_bucket(float* sums, int bucket, float sum
 }
 
 // =====================================================================================
-// Forward.  A block of 64 queries: 2 groups of 32 x (2 NT) parts of the keys of a step, NT tiles of 64; every wave keeps
-// its own online softmax and the parts are merged through LDS at the end.  WIDE: 128 queries, a wave takes 32 of them and
-// whole tiles.
+// Forward.  A block of 64 queries: 2 groups of 32 x 2 halves of every tile of 64 keys; every wave keeps its own online
+// softmax, and the halves are merged through LDS at the end.  WIDE: a wave takes 32 queries and whole tiles, half the loads
+// and barriers per product and nothing to merge: 1: 128 queries of a head, 2: 64 queries of two heads that share keys.
 // =====================================================================================
-template <class P, int NT, bool WIDE, bool BIAS>
-__global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_fwd_kernel(PackedArgs a) {
+template <class P, int WIDE, bool BIAS>
+__global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_fwd_kernel(PackedArgs a) {
     typedef typename P::elem elem;
-    constexpr int NW = 4 * NT, NSUB = WIDE ? 1 : 2 * NT, DT = P::DT;
-    constexpr int QB = WIDE ? 128 : 64, NH = WIDE ? 2 : 1;
-    constexpr int TILE = P::TILE, STAGE = NT * 2 * TILE;
+    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64, NH = WIDE ? 2 : 1;
+    constexpr int NW = 4, DT = P::DT, TILE = P::TILE, STAGE = 2 * TILE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qg = wave / NSUB, sub = wave % NSUB, tj = sub >> 1, kh = sub & 1;
+    const int hw = HP == 2 ? wave >> 1 : 0, qg = HP == 2 ? wave & 1 : WIDE ? wave : wave >> 1, kh = WIDE ? 0 : wave & 1;
     int blk, head, kvh;
-    packed_coords(a, blockIdx.x, (a.T + QB - 1) / QB, true, blk, head, kvh);
+    packed_coords<HP>(a, blockIdx.x, (a.T + QB - 1) / QB, blk, head, kvh);
+    const int head0 = head;
+    head += hw;
     const int q_wave = blk * QB + qg * 32, q_lane = q_wave + (lane & 31);
     const elem* kbase = (const elem*)a.k + kvh * a.d;
     const elem* vbase = (const elem*)a.v + kvh * a.d;
@@ -343,23 +351,19 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
     P::load(qf, (const elem*)a.q + (size_t)min(q_lane, a.T - 1) * a.ld_q + head * a.d, h, a.d);
     const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
     if (!x.blk_hi) return;
-    const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0, nsteps = (nt + NT - 1) / NT;
+    const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
     const float c = a.scale * P::kUnit;
     RelLds rel{};
-    if constexpr (BIAS) rel = rel_init<P, NW>(a, smem + 2 * STAGE, head, wave);
+    if constexpr (BIAS) rel = rel_init<P, NW, HP>(a, smem + 2 * STAGE, head0, hw, wave);
 
     TileLoader<P, NW> lk, lv;
     lk.init(wave, lane, a.ld_k, a.d);
     lv.init(wave, lane, a.ld_v, a.d);
-    auto request = [&](int step) {
-        char* st = smem + (step & 1) * STAGE;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int r0 = (t0 + step * NT + j) * 64;
-            if (step * NT + j >= nt) break;
-            lk.issue(kbase + (size_t)r0 * a.ld_k, a.ld_k, a.d, x.blk_lo - r0, x.blk_hi - r0, st + j * 2 * TILE, wave);
-            lv.issue(vbase + (size_t)r0 * a.ld_v, a.ld_v, a.d, x.blk_lo - r0, x.blk_hi - r0, st + j * 2 * TILE + TILE, wave);
-        }
+    auto request = [&](int t) {
+        char* st = smem + (t & 1) * STAGE;
+        const int r0 = (t0 + t) * 64;
+        lk.issue(kbase + (size_t)r0 * a.ld_k, a.ld_k, a.d, x.blk_lo - r0, x.blk_hi - r0, st, wave);
+        lv.issue(vbase + (size_t)r0 * a.ld_v, a.ld_v, a.d, x.blk_lo - r0, x.blk_hi - r0, st + TILE, wave);
     };
 
     f32x16 ot[DT];
@@ -369,13 +373,12 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
         m = -INFINITY;
         lsum = 0.f;
         request(0);
-        for (int t = 0; t < nsteps; ++t) {
+        for (int t = 0; t < nt; ++t) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
-            if (t + 1 < nsteps) request(t + 1);
-            const int tile = t * NT + tj, kw = (t0 + tile) * 64 + 32 * kh;
-            if (NT > 1 && tile >= nt) continue;
-            const char* sk = smem + (t & 1) * STAGE + tj * 2 * TILE;
+            if (t + 1 < nt) request(t + 1);
+            const int kw = (t0 + t) * 64 + 32 * kh;
+            const char* sk = smem + (t & 1) * STAGE;
             const char* sv = sk + TILE;
             f32x16 s[NH];
             clear<NH>(s);
@@ -454,42 +457,28 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(ot))) walk(std::true_type{});
 
-    // waves 1 .. NSUB - 1 of a query group hand (m, l, O^T) to wave 0 through LDS; a part may have seen nothing
     float l = halves_sum(lsum), mm = m;
-    if constexpr (!WIDE) {
+    if constexpr (!WIDE) {                  // the waves of the second halves hand (m, l, O^T) over; a half may have seen nothing
         __syncthreads();
-        constexpr int XO = DT * 16 * 64 + 128;
-        float* xo = (float*)smem + (size_t)qg * (NSUB - 1) * XO;
-        if (sub != 0) {
-            float* mine = xo + (size_t)(sub - 1) * XO;
+        float* xo = (float*)smem + qg * (DT * 16 * 64 + 128);
+        if (kh) {
 #pragma unroll
             for (int t2 = 0; t2 < DT; ++t2)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mine[(t2 * 16 + v) * 64 + lane] = ot[t2][v];
-            mine[DT * 16 * 64 + lane] = m;
-            mine[DT * 16 * 64 + 64 + lane] = l;
+                for (int v = 0; v < 16; ++v) xo[(t2 * 16 + v) * 64 + lane] = ot[t2][v];
+            xo[DT * 16 * 64 + lane] = m;
+            xo[DT * 16 * 64 + 64 + lane] = l;
         }
         __syncthreads();
-        if (sub != 0) return;
-#pragma unroll
-        for (int j = 0; j < NSUB - 1; ++j) mm = fmaxf(mm, xo[(size_t)j * XO + DT * 16 * 64 + lane]);
-        const float use = mm == -INFINITY ? 0.f : mm;
-        const float a0 = P::expo(m - use);
-        l *= a0;
+        if (kh) return;
+        const float m1 = xo[DT * 16 * 64 + lane];
+        mm = fmaxf(m, m1);
+        const float use = mm == -INFINITY ? 0.f : mm, a0 = P::expo(m - use), a1 = P::expo(m1 - use);
+        l = l * a0 + xo[DT * 16 * 64 + 64 + lane] * a1;
 #pragma unroll
         for (int t2 = 0; t2 < DT; ++t2)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) ot[t2][v] *= a0;
-#pragma unroll
-        for (int j = 0; j < NSUB - 1; ++j) {
-            const float* other = xo + (size_t)j * XO;
-            const float aj = P::expo(other[DT * 16 * 64 + lane] - use);
-            l += other[DT * 16 * 64 + 64 + lane] * aj;
-#pragma unroll
-            for (int t2 = 0; t2 < DT; ++t2)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) ot[t2][v] += other[(t2 * 16 + v) * 64 + lane] * aj;
-        }
+            for (int v = 0; v < 16; ++v) ot[t2][v] = ot[t2][v] * a0 + xo[(t2 * 16 + v) * 64 + lane] * a1;
     }
     if (x.hi <= x.lo) return;
     const float inv = 1.f / l;
@@ -519,18 +508,20 @@ __global__ __launch_bounds__(256 * NT, NT == 1 && P::D * sizeof(typename P::elem
 constexpr int kShort = 4;
 template <int NW> constexpr size_t table_lds() { return (size_t)NW * (8 * kSkewPitch + kMaxBuckets + kWindow) * sizeof(float); }
 
-template <class P, bool WIDE, bool BIAS>
+template <class P, int WIDE, bool BIAS>
 __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dq_kernel(PackedArgs a) {
     typedef typename P::elem elem;
-    constexpr int NW = 4, DT = P::DT, QB = WIDE ? 128 : 64, TILE = P::TILE, STAGE = 2 * TILE;
-    constexpr int NH = WIDE ? 2 : 1;
+    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64, NH = WIDE ? 2 : 1;
+    constexpr int NW = 4, DT = P::DT, TILE = P::TILE, STAGE = 2 * TILE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qg = WIDE ? wave : wave >> 1, kh0 = WIDE ? 0 : wave & 1;
+    const int hw = HP == 2 ? wave >> 1 : 0, qg = HP == 2 ? wave & 1 : WIDE ? wave : wave >> 1, kh0 = WIDE ? 0 : wave & 1;
     int blk, head, kvh;
-    packed_coords(a, blockIdx.x, (a.T + QB - 1) / QB, true, blk, head, kvh);
+    packed_coords<HP>(a, blockIdx.x, (a.T + QB - 1) / QB, blk, head, kvh);
+    const int head0 = head;
+    head += hw;
     const int q_wave = blk * QB + qg * 32, q_lane = q_wave + (lane & 31), q_src = min(q_lane, a.T - 1);
     const elem* kbase = (const elem*)a.k + kvh * a.d;
     const elem* vbase = (const elem*)a.v + kvh * a.d;
@@ -546,10 +537,14 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     }
     const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
     const bool grad = BIAS && a.table_part;
+    // partial sums of the table's gradient: of 64 rows of a head, two of them in a wide block
+    auto put_part = [&](int u, float v) {
+        const int tile = WIDE == 1 ? 2 * blk + u : blk, of = WIDE == 2 ? head0 + u : head0;
+        if (tile < (a.T + 63) / 64) a.table_part[((size_t)tile * a.heads + of) * a.rel.buckets + threadIdx.x] = v;
+    };
     if (!x.blk_hi) {
         if (grad && threadIdx.x < a.rel.buckets)
-            for (int i = 0; i < QB / 64 && blk * (QB / 64) + i < (a.T + 63) / 64; ++i)
-                a.table_part[((size_t)(blk * (QB / 64) + i) * a.heads + head) * a.rel.buckets + threadIdx.x] = 0.f;
+            for (int u = 0; u < (WIDE ? 2 : 1); ++u) put_part(u, 0.f);
         return;
     }
     const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
@@ -565,8 +560,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             delta = 0.f;
             lse = INFINITY;
         }
-        rel = rel_init<P, NW>(a, smem + 2 * STAGE, head, wave);
-        float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW>());
+        rel = rel_init<P, NW, HP>(a, smem + 2 * STAGE, head0, hw, wave);
+        float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW, HP>());
         skew = tg + wave * 8 * kSkewPitch;
         sums = tg + NW * 8 * kSkewPitch + wave * kMaxBuckets;
         near = tg + NW * (8 * kSkewPitch + kMaxBuckets) + wave * kWindow;
@@ -667,7 +662,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!WIDE) {          // two waves have half the keys of a row each
-                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW>() : 0));         // the place of `skew`
+                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW, HP>() : 0));      // the place of `skew`
                 ex[wave * 64 + lane] = delta;
                 __syncthreads();
                 delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
@@ -688,15 +683,14 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 
     __syncthreads();
     if (grad && threadIdx.x < a.rel.buckets) {
-        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW>()) + NW * 8 * kSkewPitch + threadIdx.x;
-        // a block of 128 rows has two partials' places
-        float part[2];
-        part[0] = WIDE ? tg[0] + tg[kMaxBuckets] : tg[0] + tg[kMaxBuckets] + tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
-        part[1] = tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
-#pragma unroll
-        for (int i = 0; i < QB / 64; ++i)
-            if (blk * (QB / 64) + i < (a.T + 63) / 64)
-                a.table_part[((size_t)(blk * (QB / 64) + i) * a.heads + head) * a.rel.buckets + threadIdx.x] = part[i];
+        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW, HP>()) + NW * 8 * kSkewPitch + threadIdx.x;
+        const float first = tg[0] + tg[kMaxBuckets], second = tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
+        if constexpr (WIDE) {
+            put_part(0, first);
+            put_part(1, second);
+        } else {
+            put_part(0, first + second);
+        }
     }
     float* xo = (float*)smem + (WIDE ? 0 : qg * (DT * 16 * 64));
     if constexpr (!WIDE) {
@@ -731,7 +725,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 //   S = Q K^T, P = exp(S - lse[q]), dP = dO V^T, dS = P (dP - delta[q]), dV^T += dO^T P, dK^T += Q^T dS
 // =====================================================================================
 template <class P, bool WIDE, bool BIAS>
-__global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dkv_kernel(PackedArgs a) {
+__global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedArgs a) {
     typedef typename P::elem elem;
     constexpr int NW = 4, DT = P::DT, KB = WIDE ? 128 : 64, TILE = P::TILE;
     constexpr int NH = WIDE ? 2 : 1;
@@ -938,27 +932,27 @@ static hipError_t allow_lds(K kern, size_t bytes, std::atomic<bool>& set) {
     return e;
 }
 
-template <class P, int NT, bool WIDE, bool BIAS>
+template <class P, int WIDE, bool BIAS>
 static hipError_t launch_fwd(const PackedArgs& a, hipStream_t s) {
-    constexpr int QB = WIDE ? 128 : 64;
-    constexpr size_t stages = (size_t)2 * NT * 2 * P::TILE + (BIAS ? rel_lds<4 * NT>() : 0);
-    constexpr size_t merge = WIDE ? 0 : (size_t)2 * (2 * NT - 1) * (P::DT * 16 * 64 + 128) * sizeof(float);
+    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64;
+    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4, HP>() : 0);
+    constexpr size_t merge = WIDE ? 0 : (size_t)2 * (P::DT * 16 * 64 + 128) * sizeof(float);
     constexpr size_t smem = std::max(stages, merge);
     static std::atomic<bool> set{false};
-    const hipError_t e = allow_lds(packed_fwd_kernel<P, NT, WIDE, BIAS>, smem, set);
+    const hipError_t e = allow_lds(packed_fwd_kernel<P, WIDE, BIAS>, smem, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_fwd_kernel<P, NT, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * a.heads), dim3(256 * NT), smem, s, a);
+    hipLaunchKernelGGL((packed_fwd_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * (a.heads / HP)), dim3(256), smem, s, a);
     return hipGetLastError();
 }
-template <class P, bool WIDE, bool BIAS>
+template <class P, int WIDE, bool BIAS>
 static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
-    constexpr int QB = WIDE ? 128 : 64;
-    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4>() + table_lds<4>() : 4 * 64 * sizeof(float));
+    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64;
+    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4, HP>() + table_lds<4>() : 4 * 64 * sizeof(float));
     constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * P::DT * 16 * 64 * sizeof(float));
     static std::atomic<bool> set{false};
     const hipError_t e = allow_lds(packed_dq_kernel<P, WIDE, BIAS>, smem, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_dq_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * a.heads), dim3(256), smem, s, a);
+    hipLaunchKernelGGL((packed_dq_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * (a.heads / HP)), dim3(256), smem, s, a);
     return hipGetLastError();
 }
 template <class P, bool WIDE, bool BIAS>

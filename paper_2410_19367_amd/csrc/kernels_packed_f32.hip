@@ -10,6 +10,7 @@ template <int DC>
 struct PackedF32 {
     typedef float elem;
     static constexpr int D = DC <= 64 ? 64 : 128, KS = DC / 8, DT = DC / 32, TILE = 64 * D * 4;
+    static constexpr int kDkvBlocks = D == 64 ? 2 : 1;
     static constexpr bool kRounds = false;
     // natural units: the difference to the reference point is taken before the change of base, so that large scores are
     // rounded relative to what is left of them
@@ -64,8 +65,8 @@ struct PackedF32 {
 
 template <class P, bool BIAS>
 static hipError_t both(const PackedArgs& a, bool back, hipStream_t s) {
-    if (!back) return launch_fwd<P, 1, false, BIAS>(a, s);
-    const hipError_t e = launch_dq<P, false, BIAS>(a, s);
+    if (!back) return launch_fwd<P, 0, BIAS>(a, s);
+    const hipError_t e = launch_dq<P, 0, BIAS>(a, s);
     return e != hipSuccess ? e : launch_dkv<P, false, BIAS>(a, s);
 }
 template <int DC>
