@@ -33,6 +33,13 @@ namespace bp {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// The lane, anew for each walk over the tiles: what one walk makes of it does not wait in registers for the next.
+__device__ __forceinline__ int lane_of(unsigned thread) {
+    int lane = thread & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // ---- what a row sees
 
 // Ranges of the sequences that rows first + lane + 64 r lie in (lo < 0: none), the same rows in every wave of a block.
@@ -369,6 +376,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     f32x16 ot[DT];
     float m, lsum;
     auto walk = [&](auto by_rows) __attribute__((always_inline)) {
+        const int lane = lane_of(threadIdx.x), h = lane >> 5;
         clear<DT>(ot);
         m = -INFINITY;
         lsum = 0.f;
@@ -581,6 +589,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     enum { DELTA, GRAD, BY_ROWS };
     auto walk_keys = [&](auto what) __attribute__((always_inline)) {
         constexpr int walk = decltype(what)::value;
+        const int lane = lane_of(threadIdx.x), h = lane >> 5;
         clear<DT>(dq);
         float far = 0.f, pdp = 0.f;         // sum of dS in pieces of one bucket; of P dP
         int far_bucket = -1;
@@ -791,6 +800,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
 
     f32x16 dk[DT], dv[DT];
     auto walk = [&](auto by_rows) __attribute__((always_inline)) {
+        const int lane = lane_of(threadIdx.x), h = lane >> 5;
         clear<DT>(dk);
         clear<DT>(dv);
         int t = 0, g1 = 0, t1 = 0, g2 = 0, t2 = 0;  // this step's tile; the next step's; the one after it
