@@ -739,6 +739,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     constexpr int NW = 4, DT = P::DT, KB = WIDE ? 128 : 64, TILE = P::TILE;
     constexpr int NH = WIDE ? 2 : 1;
     constexpr int STAGE = 2 * TILE + 512 + (BIAS ? kMaxBuckets * 4 : 0);       // Q, dO, -lse[64], -delta[64], the head's values
+    constexpr int KL = P::kKeysInLds ? P::kKeysInLds - BIAS : 0;        // (two blocks of a CU share 160 KB)
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
@@ -770,6 +771,9 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     TileLoader<P, NW> lq, lo;
     lq.init(wave, lane, a.ld_q, a.d);
     lo.init(wave, lane, a.ld_o, a.d);
+    char* keys = smem + 2 * STAGE + (BIAS ? (kMaxBuckets + 2 * kWindow + 4 * 64) * 4 : 0) + kg * KL * 1024;
+    if constexpr (KL > 0)
+        if (qh0 == 0) P::template put_rows<KL>(kf, keys, lane);
     // Step i takes tile t0 + i % nt of head head0 + i / nt.  Statistics (waves 0 and 1) and the head's values go through
     // registers, where they get the sign and the base that the exponential and the accumulators want; they are fetched two
     // steps ahead, so that nothing waits for them but the wait at the top of a step.
@@ -837,7 +841,8 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
                 f32x16 s, dp;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = ndlt[piece_row(v, h)]; }
-                P::scores2(sq, sdo, 32 * qh, lane, kf, vf, s, dp);
+                if constexpr (KL > 0) P::template scores2<KL>(sq, sdo, 32 * qh, lane, keys, kf, vf, s, dp);
+                else P::scores2(sq, sdo, 32 * qh, lane, kf, vf, s, dp);
                 float f = c, o = 0.f;
                 if constexpr (BIAS) {
                     int bucket;
@@ -968,7 +973,8 @@ static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
 template <class P, bool WIDE, bool BIAS>
 static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
     constexpr int KB = WIDE ? 128 : 64;
-    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + (2 * kWindow + 4 * 64) * sizeof(float) : 0);
+    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + (2 * kWindow + 4 * 64) * sizeof(float) : 0) +
+                              (P::kKeysInLds ? (P::kKeysInLds - BIAS) * 2 * 1024 : 0);
     constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
     static std::atomic<bool> set{false};
     const hipError_t e = allow_lds(packed_dkv_kernel<P, WIDE, BIAS>, smem, set);

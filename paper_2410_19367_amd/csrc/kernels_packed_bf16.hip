@@ -11,8 +11,9 @@ template <int DC>
 struct PackedBf16 {
     typedef bf16_t elem;
     static constexpr int D = DC <= 64 ? 64 : 128, KS = DC / 16, DT = DC / 32, TILE = 64 * D * 2;
-    // dK/dV blocks of 128 columns want 390 to 450 registers a lane: one block to a CU
-    static constexpr int kDkvBlocks = DC == 128 ? 1 : 2;
+    static constexpr int kDkvBlocks = 2;
+    // dK/dV: steps of the scores' contraction whose half of the keys stays in LDS, 2 KB each, where registers are short
+    static constexpr int kKeysInLds = DC == 128 ? 6 : 0;
     static constexpr bool kRounds = true;               // ctx is rounded
     static constexpr float kUnit = kLog2e, kBit = 1.f, kToNatural = kLn2;      // scores in units of a binary order
     static __device__ __forceinline__ float expo(float x) { return fast_exp2(x); }
@@ -51,6 +52,22 @@ struct PackedBf16 {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<D>(ta, row0, k, lane), a.f[k], s, 0, 0, 0);
+            p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<D>(tb, row0, k, lane), b.f[k], p, 0, 0, 0);
+        }
+    }
+    // the same with the first KL steps of a in LDS, as put_rows left them
+    template <int KL>
+    static __device__ __forceinline__ void put_rows(const Rows& a, char* lds, int lane) {
+#pragma unroll
+        for (int k = 0; k < KL; ++k) *reinterpret_cast<bf16x8*>(lds + k * 1024 + lane * 16) = a.f[k];
+    }
+    template <int KL>
+    static __device__ __forceinline__ void scores2(const char* ta, const char* tb, int row0, int lane, const char* lds, const Rows& a,
+                                                   const Rows& b, f32x16& s, f32x16& p) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const bf16x8 ak = k < KL ? *reinterpret_cast<const bf16x8*>(lds + k * 1024 + lane * 16) : a.f[k];
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<D>(ta, row0, k, lane), ak, s, 0, 0, 0);
             p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<D>(tb, row0, k, lane), b.f[k], p, 0, 0, 0);
         }
     }
@@ -118,8 +135,6 @@ static hipError_t bwd(const PackedArgs& a, hipStream_t s) {
     if constexpr (BIAS) e = launch_dq<P, 0, BIAS>(a, s);
     else e = wide_dq(a) ? launch_dq<P, 2, BIAS>(a, s) : launch_dq<P, 0, BIAS>(a, s);
     if (e != hipSuccess) return e;
-    if constexpr (P::kDkvBlocks == 1)
-        if (wide_dkv(a)) return launch_dkv<P, true, BIAS>(a, s);
     return launch_dkv<P, false, BIAS>(a, s);
 }
 template <int DC>

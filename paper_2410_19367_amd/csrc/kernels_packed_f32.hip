@@ -10,7 +10,7 @@ template <int DC>
 struct PackedF32 {
     typedef float elem;
     static constexpr int D = DC <= 64 ? 64 : 128, KS = DC / 8, DT = DC / 32, TILE = 64 * D * 4;
-    static constexpr int kDkvBlocks = D == 64 ? 2 : 1;
+    static constexpr int kDkvBlocks = D == 64 ? 2 : 1, kKeysInLds = 0;
     static constexpr bool kRounds = false;
     // natural units: the difference to the reference point is taken before the change of base, so that large scores are
     // rounded relative to what is left of them
