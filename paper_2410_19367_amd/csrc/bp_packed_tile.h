@@ -244,6 +244,15 @@ __device__ __forceinline__ float sum_by_offset(float* skew, const f32x16& x, int
     return sum;
 }
 
+// step(i, slot) for i < n, i in stage i % 2: with the stage a constant, its LDS offset is part of the instructions
+template <class S>
+__device__ __forceinline__ void two_by_two(int n, S step) {
+    for (int i = 0; i < n; i += 2) {
+        step(i, std::integral_constant<int, 0>{});
+        if (i + 1 < n) step(i + 1, std::integral_constant<int, 1>{});
+    }
+}
+
 // ---- the bias of a piece
 //
 // A piece of 32 x 32 pairs has 63 offsets.  Far from the diagonal they share a bucket, and the bias is one number that
@@ -381,12 +390,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         m = -INFINITY;
         lsum = 0.f;
         request(0);
-        for (int t = 0; t < nt; ++t) {
+        auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+            constexpr int slot = decltype(odd)::value;
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (t + 1 < nt) request(t + 1);
             const int kw = (t0 + t) * 64 + 32 * kh;
-            const char* sk = smem + (t & 1) * STAGE;
+            const char* sk = smem + slot * STAGE;
             const char* sv = sk + TILE;
             f32x16 s[NH];
             clear<NH>(s);
@@ -460,7 +470,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 else
                     P::contract(sv, 32 * (kh + u), lane, s[u], ot);
             }
-        }
+        };
+        two_by_two(nt, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(ot))) walk(std::true_type{});
