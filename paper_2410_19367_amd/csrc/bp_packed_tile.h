@@ -616,11 +616,12 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             for (int i = lane; i < 8 * kSkewPitch; i += 64) skew[i] = 0.f;
         }
         request(0);
-        for (int t = 0; t < nt; ++t) {
+        auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+            constexpr int slot = decltype(odd)::value;
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (t + 1 < nt) request(t + 1);
-            const char* sk = smem + (t & 1) * STAGE;
+            const char* sk = smem + slot * STAGE;
             const char* sv = sk + TILE;
 #pragma unroll
             for (int kh = kh0; kh < kh0 + NH; ++kh) {
@@ -678,7 +679,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 if constexpr (walk == BY_ROWS) contract_by_rows<P>(sk, 32 * kh, lane, x.lo - kw, x.hi - kw, dp, dq);
                 else P::contract(sk, 32 * kh, lane, dp, dq);
             }
-        }
+        };
+        two_by_two(nt, step);
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!WIDE) {          // two waves have half the keys of a row each
@@ -824,25 +826,26 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
         float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1), win1 = fetch_win(g1);
         request(0, 0, smem);
         put(st0, tab0, win0, 0);
-        for (int i = 0; i < steps; ++i) {
+        auto step = [&](int i, auto odd) __attribute__((always_inline)) {
+            constexpr int slot = decltype(odd)::value;
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (i + 1 < steps) {
                 put(st1, tab1, win1, i + 1);
-                request(g1, t1, smem + ((i + 1) & 1) * STAGE);
+                request(g1, t1, smem + (1 - slot) * STAGE);
                 g2 = g1; t2 = t1;
                 advance(g2, t2);
                 st1 = fetch_stat(g2, t2);
                 tab1 = fetch_tab(g2);
                 win1 = fetch_win(g2);
             }
-            const char* sq = smem + (i & 1) * STAGE;
+            const char* sq = smem + slot * STAGE;
             const char* sdo = sq + TILE;
             const int q0 = (t0 + t) * 64;
             t = t1; g1 = g2; t1 = t2;
             if constexpr (BIAS) {
                 rel.tab = (const float*)(sq + 2 * TILE + 512);
-                rel.win = wins + (i & 1) * kWindow;
+                rel.win = wins + slot * kWindow;
             }
 #pragma unroll
             for (int qh = qh0; qh < qh0 + NH; ++qh) {
@@ -890,7 +893,8 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
                     P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
                 }
             }
-        }
+        };
+        two_by_two(steps, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && (any_nan<DT>(dk) || any_nan<DT>(dv)))) walk(std::true_type{});
