@@ -404,9 +404,10 @@ int bp_op_attention_bwd(int dtype, int B, int S, int heads, int head_dim, int ca
  *     lse[i] = log sum_j exp z[i][j]          ctx[i] = sum_j exp(z[i][j] - lse[i]) v[j]
  * Row t, head h, element c of a tensor lies at t * ld + h * head_dim + c; gradients lie as the tensors they belong to
  * (dq as q, dk as k, dv as v, dctx as ctx).  bf16 products take the probabilities and the score gradients rounded to
- * bf16; sums and softmax are fp32. */
+ * bf16; sums and softmax are fp32.  A value that is not finite reaches only what depends on it: other sequences, and
+ * earlier tokens under a causal mask, keep their results.  Results must not overlap inputs or each other. */
 typedef struct {
-    int tokens;             /* rows of every tensor, below 2^24                                      */
+    int tokens;             /* rows of every tensor, below 2^24; (tokens + 63) / 64 * heads, too     */
     int sequences;          /* >= 1                                                                  */
     const int32_t* starts;  /* dev [sequences + 1], ascending, within 0 .. tokens                    */
     int heads, kv_heads;    /* heads a multiple of kv_heads                                          */
@@ -423,7 +424,8 @@ typedef struct {
 typedef struct {
     int buckets;            /* causal: 2 .. 128; else even, 4 .. 128                                 */
     int max_distance;       /* above e, below 2^24                                                   */
-    const float* table;     /* dev fp32 [buckets, heads]                                             */
+    const float* table;     /* dev fp32 [buckets, heads]; -inf (or a value next to the type's lowest) */
+                            /* takes a bucket out; a query with nothing else gets NaN                */
 } bp_relpos;
 
 /* Bucket of offset = key position - query position (pure CPU); BP_EINVAL for what the fields above do not allow. */

@@ -85,6 +85,9 @@ int make_args(int dtype, const bp_packed* p, const bp_relpos* bias, PackedArgs& 
         return fail(BP_EINVAL, "leading dimension smaller than the row length");
     if (a.ld_q >= 1 << 24 || a.ld_k >= 1 << 24 || a.ld_v >= 1 << 24 || a.ld_o >= 1 << 24)
         return fail(BP_ESHAPE, "leading dimensions must be below 2^24");
+    // (a launch has fewer than 2^32 threads)
+    if ((int64_t)packed_tiles(a.T) * a.heads >= 1 << 24)
+        return fail(BP_ESHAPE, "%d tokens of %d heads: (tokens + 63) / 64 * heads must be below 2^24", a.T, a.heads);
     if (bias) {
         if (!bias->table) return fail(BP_EINVAL, "null bias table");
         const int rc = make_relpos(a.causal, bias->buckets, bias->max_distance, a.rel);

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 }
 
 // =====================================================================================
-// dQ, and delta for dK/dV.  Decomposed as the forward:
+// dQ, and delta for dK/dV.  Decomposed as the forward (PAIR: 64 queries of two heads that share keys):
 //   S^T = K Q^T, P^T = exp(S^T - lse), dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T
 // delta = dO . ctx, or the sum of P dP over a first walk of the keys where the rounding of ctx to bf16 would be felt:
 //   the table's gradient is wanted: the last buckets' sums are small differences of many pairs (half a percent of them came
@@ -527,19 +527,19 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 constexpr int kShort = 4;
 template <int NW> constexpr size_t table_lds() { return (size_t)NW * (8 * kSkewPitch + kMaxBuckets + kWindow) * sizeof(float); }
 
-template <class P, int WIDE, bool BIAS>
+template <class P, bool PAIR, bool BIAS>
 __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1) void packed_dq_kernel(PackedArgs a) {
+    static_assert(!(PAIR && BIAS), "the table's gradient: one head a block");
     typedef typename P::elem elem;
-    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64, NH = WIDE ? 2 : 1;
+    constexpr int HP = PAIR ? 2 : 1, QB = 64, NH = PAIR ? 2 : 1;
     constexpr int NW = 4, DT = P::DT, TILE = P::TILE, STAGE = 2 * TILE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hw = HP == 2 ? wave >> 1 : 0, qg = HP == 2 ? wave & 1 : WIDE ? wave : wave >> 1, kh0 = WIDE ? 0 : wave & 1;
+    const int hw = PAIR ? wave >> 1 : 0, qg = PAIR ? wave & 1 : wave >> 1, kh0 = PAIR ? 0 : wave & 1;
     int blk, head, kvh;
     packed_coords<HP>(a, blockIdx.x, (a.T + QB - 1) / QB, blk, head, kvh);
-    const int head0 = head;
     head += hw;
     const int q_wave = blk * QB + qg * 32, q_lane = q_wave + (lane & 31), q_src = min(q_lane, a.T - 1);
     const elem* kbase = (const elem*)a.k + kvh * a.d;
@@ -556,14 +556,9 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     }
     const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
     const bool grad = BIAS && a.table_part;
-    // partial sums of the table's gradient: of 64 rows of a head, two of them in a wide block
-    auto put_part = [&](int u, float v) {
-        const int tile = WIDE == 1 ? 2 * blk + u : blk, of = WIDE == 2 ? head0 + u : head0;
-        if (tile < (a.T + 63) / 64) a.table_part[((size_t)tile * a.heads + of) * a.rel.buckets + threadIdx.x] = v;
-    };
+    auto put_part = [&](float v) { a.table_part[((size_t)blk * a.heads + head) * a.rel.buckets + threadIdx.x] = v; };
     if (!x.blk_hi) {
-        if (grad && threadIdx.x < a.rel.buckets)
-            for (int u = 0; u < (WIDE ? 2 : 1); ++u) put_part(u, 0.f);
+        if (grad && threadIdx.x < a.rel.buckets) put_part(0.f);
         return;
     }
     const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
@@ -579,8 +574,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             delta = 0.f;
             lse = INFINITY;
         }
-        rel = rel_init<P, NW, HP>(a, smem + 2 * STAGE, head0, hw, wave);
-        float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW, HP>());
+        rel = rel_init<P, NW, 1>(a, smem + 2 * STAGE, head, 0, wave);
+        float* tg = (float*)(smem + 2 * STAGE + rel_lds<NW, 1>());
         skew = tg + wave * 8 * kSkewPitch;
         sums = tg + NW * 8 * kSkewPitch + wave * kMaxBuckets;
         near = tg + NW * (8 * kSkewPitch + kMaxBuckets) + wave * kWindow;
@@ -683,8 +678,8 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         two_by_two(nt, step);
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
-            if constexpr (!WIDE) {          // two waves have half the keys of a row each
-                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW, HP>() : 0));      // the place of `skew`
+            if constexpr (!PAIR) {          // two waves have half the keys of a row each
+                float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW, 1>() : 0));      // the place of `skew`
                 ex[wave * 64 + lane] = delta;
                 __syncthreads();
                 delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
@@ -705,17 +700,11 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 
     __syncthreads();
     if (grad && threadIdx.x < a.rel.buckets) {
-        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW, HP>()) + NW * 8 * kSkewPitch + threadIdx.x;
-        const float first = tg[0] + tg[kMaxBuckets], second = tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets];
-        if constexpr (WIDE) {
-            put_part(0, first);
-            put_part(1, second);
-        } else {
-            put_part(0, first + second);
-        }
+        const float* tg = (const float*)(smem + 2 * STAGE + rel_lds<NW, 1>()) + NW * 8 * kSkewPitch + threadIdx.x;
+        put_part(tg[0] + tg[kMaxBuckets] + (tg[2 * kMaxBuckets] + tg[3 * kMaxBuckets]));
     }
-    float* xo = (float*)smem + (WIDE ? 0 : qg * (DT * 16 * 64));
-    if constexpr (!WIDE) {
+    float* xo = (float*)smem + (PAIR ? 0 : qg * (DT * 16 * 64));
+    if constexpr (!PAIR) {
         if (kh0 == 1) {
 #pragma unroll
             for (int t2 = 0; t2 < DT; ++t2)
@@ -734,30 +723,29 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             f32x4 w;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                w[e] = (WIDE ? dq[t2][4 * g + e] : dq[t2][4 * g + e] + xo[(t2 * 16 + 4 * g + e) * 64 + lane]) * a.scale;
+                w[e] = (PAIR ? dq[t2][4 * g + e] : dq[t2][4 * g + e] + xo[(t2 * 16 + 4 * g + e) * 64 + lane]) * a.scale;
             const int col = t2 * 32 + 8 * g + 4 * h;
             if (col < a.d) P::store(out + col, w);
         }
 }
 
 // =====================================================================================
-// dK and dV of 64 keys (WIDE: 128) of a key / value head: 2 groups of 32 keys x 2 halves of every tile of 64 queries, the
-// tiles of the heads that share them one after the other: all of them, or with a.splits > 1 an equal part, whose fp32 sums
+// dK and dV of 64 keys of a key / value head: 2 groups of 32 keys x 2 halves of every tile of 64 queries, the tiles of the
+// heads that share them one after the other: all of them, or with a.splits > 1 an equal part, whose fp32 sums
 // go to the workspace and are joined in a fixed order by packed_join_kernel (split_heads).
 //   S = Q K^T, P = exp(S - lse[q]), dP = dO V^T, dS = P (dP - delta[q]), dV^T += dO^T P, dK^T += Q^T dS
 // =====================================================================================
-template <class P, bool WIDE, bool BIAS>
+template <class P, bool BIAS>
 __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedArgs a) {
     typedef typename P::elem elem;
-    constexpr int NW = 4, DT = P::DT, KB = WIDE ? 128 : 64, TILE = P::TILE;
-    constexpr int NH = WIDE ? 2 : 1;
+    constexpr int NW = 4, DT = P::DT, KB = 64, TILE = P::TILE;
     constexpr int STAGE = 2 * TILE + 512 + (BIAS ? kMaxBuckets * 4 : 0);       // Q, dO, -lse[64], -delta[64], the head's values
     constexpr int KL = P::kKeysInLds ? P::kKeysInLds - BIAS : 0;        // (two blocks of a CU share 160 KB)
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kg = WIDE ? wave : wave >> 1, qh0 = WIDE ? 0 : wave & 1;
+    const int kg = wave >> 1, qh = wave & 1;
     const int G = a.heads / a.kv_heads / a.splits;                      // heads of this block
     const int blk = blockIdx.x / (a.kv_heads * a.splits);               // the first rows have most to do
     const int part = (blockIdx.x - blk * a.kv_heads * a.splits) / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
@@ -786,7 +774,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     lo.init(wave, lane, a.ld_o, a.d);
     char* keys = smem + 2 * STAGE + (BIAS ? (kMaxBuckets + 2 * kWindow + 4 * 64) * 4 : 0) + kg * KL * 1024;
     if constexpr (KL > 0)
-        if (qh0 == 0) P::template put_rows<KL>(kf, keys, lane);
+        if (qh == 0) P::template put_rows<KL>(kf, keys, lane);
     // Step i takes tile t0 + i % nt of head head0 + i / nt.  Statistics (waves 0 and 1) and the head's values go through
     // registers, where they get the sign and the base that the exponential and the accumulators want; they are fetched two
     // steps ahead, so that nothing waits for them but the wait at the top of a step.
@@ -847,72 +835,67 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
                 rel.tab = (const float*)(sq + 2 * TILE + 512);
                 rel.win = wins + slot * kWindow;
             }
+            const int qw = q0 + 32 * qh;
+            const float* nlse = (const float*)(sq + 2 * TILE) + 32 * qh;
+            const float* ndlt = nlse + 64;
+            f32x16 s, dp;
 #pragma unroll
-            for (int qh = qh0; qh < qh0 + NH; ++qh) {
-                const int qw = q0 + 32 * qh;
-                const float* nlse = (const float*)(sq + 2 * TILE) + 32 * qh;
-                const float* ndlt = nlse + 64;
-                f32x16 s, dp;
+            for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = ndlt[piece_row(v, h)]; }
+            if constexpr (KL > 0) P::template scores2<KL>(sq, sdo, 32 * qh, lane, keys, kf, vf, s, dp);
+            else P::scores2(sq, sdo, 32 * qh, lane, kf, vf, s, dp);
+            float f = c, o = 0.f;
+            if constexpr (BIAS) {
+                int bucket;
+                float value;
+                const float* b;
+                if (bias_of_piece(a.rel, rel, a.causal, k_wave - qw - 31, lane, value, bucket, b) != ONE_BUCKET) {
+                    b += 31 + (lane & 31) - 4 * h - 27;         // offsets fall with the register's row, 0 .. 27 here
 #pragma unroll
-                for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = ndlt[piece_row(v, h)]; }
-                if constexpr (KL > 0) P::template scores2<KL>(sq, sdo, 32 * qh, lane, keys, kf, vf, s, dp);
-                else P::scores2(sq, sdo, 32 * qh, lane, kf, vf, s, dp);
-                float f = c, o = 0.f;
-                if constexpr (BIAS) {
-                    int bucket;
-                    float value;
-                    const float* b;
-                    if (bias_of_piece(a.rel, rel, a.causal, k_wave - qw - 31, lane, value, bucket, b) != ONE_BUCKET) {
-                        b += 31 + (lane & 31) - 4 * h - 27;         // offsets fall with the register's row, 0 .. 27 here
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[27 - 8 * (v >> 2) - (v & 3)]);
-                        f = 1.f;
-                    } else {
-                        o = value;
-                    }
-                }
-                const bool masked = qw < x.inner_lo || qw + 32 > x.inner_hi;
-                if (masked) {
-                    asm volatile("");
-#pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if ((unsigned)(qw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {
-                            s[v] = -INFINITY;
-                            if (decltype(by_rows)::value) dp[v] = 0.f;
-                        }
-                }
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    s[v] = P::expo(__builtin_fmaf(s[v], f, BIAS ? nlse[piece_row(v, h)] + o : nlse[piece_row(v, h)]));     // P
-                    dp[v] *= s[v];                                                                                        // dS
-                }
-                if constexpr (decltype(by_rows)::value) {
-                    contract_by_rows<P>(sdo, 32 * qh, lane, x.lo - qw, x.hi - qw, s, dv);
-                    contract_by_rows<P>(sq, 32 * qh, lane, x.lo - qw, x.hi - qw, dp, dk);
+                    for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, b[27 - 8 * (v >> 2) - (v & 3)]);
+                    f = 1.f;
                 } else {
-                    P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
+                    o = value;
                 }
+            }
+            const bool masked = qw < x.inner_lo || qw + 32 > x.inner_hi;
+            if (masked) {
+                asm volatile("");
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if ((unsigned)(qw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {
+                        s[v] = -INFINITY;
+                        if (decltype(by_rows)::value) dp[v] = 0.f;
+                    }
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[v] = P::expo(__builtin_fmaf(s[v], f, BIAS ? nlse[piece_row(v, h)] + o : nlse[piece_row(v, h)]));     // P
+                dp[v] *= s[v];                                                                                        // dS
+            }
+            if constexpr (decltype(by_rows)::value) {
+                contract_by_rows<P>(sdo, 32 * qh, lane, x.lo - qw, x.hi - qw, s, dv);
+                contract_by_rows<P>(sq, 32 * qh, lane, x.lo - qw, x.hi - qw, dp, dk);
+            } else {
+                P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
             }
         };
         two_by_two(steps, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && (any_nan<DT>(dk) || any_nan<DT>(dv)))) walk(std::true_type{});
-    float* xo = (float*)smem + (WIDE ? 0 : kg * (2 * DT * 16 * 64));
-    if constexpr (!WIDE) {
-        __syncthreads();
-        if (qh0 == 1) {
+    float* xo = (float*)smem + kg * (2 * DT * 16 * 64);
+    __syncthreads();
+    if (qh == 1) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    xo[(t * 16 + v) * 64 + lane] = dk[t][v];
-                    xo[((DT + t) * 16 + v) * 64 + lane] = dv[t][v];
-                }
-        }
-        __syncthreads();
-        if (qh0 == 1) return;
+            for (int v = 0; v < 16; ++v) {
+                xo[(t * 16 + v) * 64 + lane] = dk[t][v];
+                xo[((DT + t) * 16 + v) * 64 + lane] = dv[t][v];
+            }
     }
+    __syncthreads();
+    if (qh == 1) return;
     if (x.hi <= x.lo) return;
     elem* dk_out = (elem*)a.dk + (size_t)k_lane * a.ld_k + kvh * a.d;
     elem* dv_out = (elem*)a.dv + (size_t)k_lane * a.ld_v + kvh * a.d;
@@ -925,8 +908,8 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
             f32x4 k4, v4;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                k4[e] = (WIDE ? dk[t][4 * g + e] : dk[t][4 * g + e] + xo[(t * 16 + 4 * g + e) * 64 + lane]) * a.scale;
-                v4[e] = WIDE ? dv[t][4 * g + e] : dv[t][4 * g + e] + xo[((DT + t) * 16 + 4 * g + e) * 64 + lane];
+                k4[e] = (dk[t][4 * g + e] + xo[(t * 16 + 4 * g + e) * 64 + lane]) * a.scale;
+                v4[e] = dv[t][4 * g + e] + xo[((DT + t) * 16 + 4 * g + e) * 64 + lane];
             }
             if (col >= a.d) continue;
             if (sums) {
@@ -954,11 +937,15 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
 
 // ---- host side
 
+// set: a bit for each device that knows
 template <typename K>
-static hipError_t allow_lds(K kern, size_t bytes, std::atomic<bool>& set) {
-    if (bytes <= 64 * 1024 || set.load(std::memory_order_acquire)) return hipSuccess;
-    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == hipSuccess) set.store(true, std::memory_order_release);
+static hipError_t allow_lds(K kern, size_t bytes, std::atomic<uint64_t>& set) {
+    if (bytes <= 64 * 1024) return hipSuccess;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess || (set.load(std::memory_order_acquire) >> (dev & 63) & 1)) return e;
+    e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess) set.fetch_or(1ull << (dev & 63), std::memory_order_release);
     return e;
 }
 
@@ -968,33 +955,31 @@ static hipError_t launch_fwd(const PackedArgs& a, hipStream_t s) {
     constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4, HP>() : 0);
     constexpr size_t merge = WIDE ? 0 : (size_t)2 * (P::DT * 16 * 64 + 128) * sizeof(float);
     constexpr size_t smem = std::max(stages, merge);
-    static std::atomic<bool> set{false};
+    static std::atomic<uint64_t> set{0};
     const hipError_t e = allow_lds(packed_fwd_kernel<P, WIDE, BIAS>, smem, set);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((packed_fwd_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * (a.heads / HP)), dim3(256), smem, s, a);
     return hipGetLastError();
 }
-template <class P, int WIDE, bool BIAS>
+template <class P, bool PAIR, bool BIAS>
 static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
-    constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64;
-    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4, HP>() + table_lds<4>() : 4 * 64 * sizeof(float));
-    constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * P::DT * 16 * 64 * sizeof(float));
-    static std::atomic<bool> set{false};
-    const hipError_t e = allow_lds(packed_dq_kernel<P, WIDE, BIAS>, smem, set);
+    constexpr size_t stages = (size_t)2 * 2 * P::TILE + (BIAS ? rel_lds<4, 1>() + table_lds<4>() : 4 * 64 * sizeof(float));
+    constexpr size_t smem = std::max(stages, PAIR ? (size_t)0 : (size_t)2 * P::DT * 16 * 64 * sizeof(float));
+    static std::atomic<uint64_t> set{0};
+    const hipError_t e = allow_lds(packed_dq_kernel<P, PAIR, BIAS>, smem, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_dq_kernel<P, WIDE, BIAS>), dim3((a.T + QB - 1) / QB * (a.heads / HP)), dim3(256), smem, s, a);
+    hipLaunchKernelGGL((packed_dq_kernel<P, PAIR, BIAS>), dim3(packed_tiles(a.T) * (a.heads / (PAIR ? 2 : 1))), dim3(256), smem, s, a);
     return hipGetLastError();
 }
-template <class P, bool WIDE, bool BIAS>
+template <class P, bool BIAS>
 static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
-    constexpr int KB = WIDE ? 128 : 64;
     constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + (2 * kWindow + 4 * 64) * sizeof(float) : 0) +
                               (P::kKeysInLds ? (P::kKeysInLds - BIAS) * 2 * 1024 : 0);
-    constexpr size_t smem = std::max(stages, WIDE ? (size_t)0 : (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
-    static std::atomic<bool> set{false};
-    const hipError_t e = allow_lds(packed_dkv_kernel<P, WIDE, BIAS>, smem, set);
+    constexpr size_t smem = std::max(stages, (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
+    static std::atomic<uint64_t> set{0};
+    const hipError_t e = allow_lds(packed_dkv_kernel<P, BIAS>, smem, set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_dkv_kernel<P, WIDE, BIAS>), dim3((a.T + KB - 1) / KB * a.kv_heads * a.splits), dim3(256), smem, s, a);
+    hipLaunchKernelGGL((packed_dkv_kernel<P, BIAS>), dim3(packed_tiles(a.T) * a.kv_heads * a.splits), dim3(256), smem, s, a);
     if (a.splits > 1) {
         const size_t threads = (size_t)a.T * (a.kv_heads * 2 * a.d / 4);
         hipLaunchKernelGGL((packed_join_kernel<P>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);

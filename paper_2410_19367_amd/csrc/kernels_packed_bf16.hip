@@ -102,7 +102,7 @@ struct PackedBf16 {
     }
 };
 
-// Which form of a kernel a launch takes.  n: blocks of 64 rows of all heads (key / value heads).  What the sequences are is
+// Which form of a kernel a launch takes.  n: blocks of 64 rows of all heads.  What the sequences are is
 // not known here, so the rules are by what holds whatever they are; measured on 256 CUs, narrow / wide, with sequences of
 // 256, 512, 1000 to 4168, 2048 and 8192 tokens:
 //   forward, d 128 (and 96): n 8192 1.20 - 1.32, 4096 1.2, 2048 1.04 - 1.3 (four long ones without a mask 0.91), 1024 with 16
@@ -110,19 +110,14 @@ struct PackedBf16 {
 //     d 64 and less: n 4096 1.0 - 1.09, 2048 0.87 - 1.13 (32 heads 1.05 - 1.28), 1024 0.8 - 1.13, fewer 0.7 - 1.0;
 //     two heads to a block against 128 rows, where both can be: 1.00 - 1.12;
 //   dQ (of the whole backward), two heads to a block: 32 heads or more, n from 2048 on 0.99 - 1.18, else 0.8 - 1.09; with the
-//     table's gradient 0.92 - 1.01;
-//   dK/dV, d 128, n with its parts: 1024 and more 1.07 - 1.18 against two narrow blocks to a CU, 0.97 - 1.19 against one;
-//     512 without a mask 1.15; else narrow (0.85); d 64 0.74 - 0.85, d 96 0.84.
+//     table's gradient 0.92 - 1.01.
 static bool wide_fwd(const PackedArgs& a) {
     const long cu = cu_count(), n = (long)packed_tiles(a.T) * a.heads;
     if (a.d > 64) return n >= (a.heads >= 16 ? 4 : 8) * cu;
     return n >= (a.heads >= 32 ? 8 : 16) * cu;
 }
-static bool wide_dq(const PackedArgs& a) {
+static bool pair_dq(const PackedArgs& a) {
     return a.heads / a.kv_heads % 2 == 0 && a.heads >= 32 && (long)packed_tiles(a.T) * a.heads >= 8L * cu_count();
-}
-static bool wide_dkv(const PackedArgs& a) {
-    return (long)packed_tiles(a.T) * a.kv_heads * a.splits >= (a.causal ? 4 : 2) * (long)cu_count();
 }
 template <class P, bool BIAS>
 static hipError_t fwd(const PackedArgs& a, hipStream_t s) {
@@ -132,10 +127,10 @@ static hipError_t fwd(const PackedArgs& a, hipStream_t s) {
 template <class P, bool BIAS>
 static hipError_t bwd(const PackedArgs& a, hipStream_t s) {
     hipError_t e;
-    if constexpr (BIAS) e = launch_dq<P, 0, BIAS>(a, s);
-    else e = wide_dq(a) ? launch_dq<P, 2, BIAS>(a, s) : launch_dq<P, 0, BIAS>(a, s);
+    if constexpr (BIAS) e = launch_dq<P, false, BIAS>(a, s);
+    else e = pair_dq(a) ? launch_dq<P, true, BIAS>(a, s) : launch_dq<P, false, BIAS>(a, s);
     if (e != hipSuccess) return e;
-    return launch_dkv<P, false, BIAS>(a, s);
+    return launch_dkv<P, BIAS>(a, s);
 }
 template <int DC>
 static hipError_t width(const PackedArgs& a, bool back, hipStream_t s) {

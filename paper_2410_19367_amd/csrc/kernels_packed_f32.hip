@@ -66,8 +66,8 @@ struct PackedF32 {
 template <class P, bool BIAS>
 static hipError_t both(const PackedArgs& a, bool back, hipStream_t s) {
     if (!back) return launch_fwd<P, 0, BIAS>(a, s);
-    const hipError_t e = launch_dq<P, 0, BIAS>(a, s);
-    return e != hipSuccess ? e : launch_dkv<P, false, BIAS>(a, s);
+    const hipError_t e = launch_dq<P, false, BIAS>(a, s);
+    return e != hipSuccess ? e : launch_dkv<P, BIAS>(a, s);
 }
 template <int DC>
 static hipError_t width(const PackedArgs& a, bool back, hipStream_t s) {

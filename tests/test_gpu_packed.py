@@ -65,7 +65,16 @@ class Call:
         return po.attention(self.starts, self.q, self.k, self.v, self.causal, self.scale, self.table, self.far,
                             dctx=self.g if want else None, ctx_given=ctx_given)
 
-    def run(self, backward=True, want_table=True, dtable0=None, stream=None):
+    def run(self, *args, **kw):
+        out = self.start(*args, **kw)
+        self.torch.cuda.synchronize()
+        return self.finish(out)
+
+    def finish(self, out):
+        host = {n: hz.to_host(t) for n, t in out.items()}
+        return {n: a if n in ("lse", "dtable") else a.reshape(self.T, -1, self.d) for n, a in host.items()}
+
+    def start(self, stream=None, backward=True, want_table=True, dtable0=None):
         bp, torch = self.bp, self.torch
         q, k, v = self.tensors(self.q, self.k, self.v)
         mark = 7.0                                       # what rows of no sequence hold afterwards
@@ -90,9 +99,7 @@ class Call:
             out |= {"dq": dq, "dk": dk, "dv": dv}
             if dtable is not None:
                 out["dtable"] = dtable
-        torch.cuda.synchronize()
-        host = {n: hz.to_host(t) for n, t in out.items()}
-        return {n: a if n in ("lse", "dtable") else a.reshape(self.T, -1, self.d) for n, a in host.items()}
+        return out
 
     def check(self, got, r=None, mark=7.0):
         if r is None:
@@ -172,6 +179,78 @@ def test_packed_every_block_shape(dtype, buckets):
             continue
         c = Call(lens, H, Hk, d, causal, dtype, back=3, buckets=buckets, far=128)
         c.check(c.run())
+
+
+# Launches with enough blocks for those of two heads and of 128 rows (on 256 CUs), of sequences that begin anywhere in them
+WIDE = [([60] * 140 + [5], 32, 8, 64, True), ([61] * 140, 32, 32, 64, False), ([60] * 140, 16, 16, 128, True),
+        ([1, 200, 61, 0, 77] * 25, 16, 8, 96, False), ([130] * 16, 32, 1, 128, True), ([3, 60, 100] * 50, 33, 11, 40, True)]
+
+
+@pytest.mark.parametrize("lens,H,Hk,d,causal", WIDE)
+@pytest.mark.parametrize("buckets", [0, 32])
+def test_packed_wide_blocks(lens, H, Hk, d, causal, buckets):
+    c = Call(lens, H, Hk, d, causal, "bf16", front=3, back=7, buckets=buckets, far=48, fused=True)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("lens,H,Hk,d,causal", WIDE[:4])
+def test_packed_wide_blocks_what_is_not_finite(lens, H, Hk, d, causal):
+    clean = Call(lens, H, Hk, d, causal, "bf16", front=3, back=7)
+    r = clean.reference()
+    c = Call(lens, H, Hk, d, causal, "bf16", front=3, back=7)
+    G, bad = H // Hk, [i for i, n in enumerate(lens) if n > 50][-2]
+    at = c.starts[bad] + 40
+    c.v[at, Hk - 1, 1] = np.nan
+    for x in (c.q, c.k, c.v, c.g):
+        x[:3] = np.nan
+        x[c.starts[-1]:] = np.nan
+    got = c.run()
+    tol = po.bounds(r, c.longest, d, G, UNIT["bf16"])
+    S = slice(c.starts[bad], c.starts[bad + 1])
+    for name in ("ctx", "dq", "dk", "dv"):
+        reach = np.zeros(got[name].shape[:2], bool)
+        if name in ("ctx", "dq"):
+            reach[slice(at, S.stop) if causal else S, H - G:] = True
+        else:
+            reach[S, Hk - 1] = True
+        fine = ~reach
+        fine[:3] = fine[c.starts[-1]:] = False
+        assert (np.abs(got[name][fine] - r[name][fine]) <= 2 * tol[name][fine] + 1e-30).all(), name
+        assert (got[name][:3] == 7.0).all() and (got[name][c.starts[-1]:] == 7.0).all()
+    assert np.isnan(got["ctx"][at, H - G:, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_least_workspace(dtype):
+    """Without room for the sums of parts, shared heads are summed in one block."""
+    import torch
+    import paper_2410_19367_amd as bp
+    c = Call([100, 70], 8, 1, 64, True, dtype, buckets=16, far=40)
+    need = ((8 * c.T + 3) & ~3) + ((c.T + 63) // 64 * 8 * 16 + 3 & ~3)
+    full = bp.bp_op_attention_packed_workspace
+    try:
+        bp.bp_op_attention_packed_workspace = lambda *a: need
+        c.check(c.run())
+    finally:
+        bp.bp_op_attention_packed_workspace = full
+    assert full(c.dt, bp.bp_packed(c.T, 2, c.starts_dev, 8, 1, 64, True), None) > 8 * c.T
+    torch.cuda.synchronize()
+
+
+def test_packed_two_calls_at_once():
+    """Two streams, a workspace each."""
+    import torch
+    a, b = Call([400, 90], 8, 2, 64, True, "bf16", buckets=32, far=64), Call([300, 33, 150], 4, 4, 128, False, "bf16")
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(streams[0]):
+            x = a.start(streams[0].cuda_stream)
+        with torch.cuda.stream(streams[1]):
+            y = b.start(streams[1].cuda_stream)
+        torch.cuda.synchronize()
+        a.check(a.finish(x))
+        b.check(b.finish(y))
 
 
 def test_packed_table_gradient_adds_and_is_optional():

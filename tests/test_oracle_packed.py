@@ -109,7 +109,7 @@ def _calls(layout, bias=None, dtype=bp.BP_BF16, missing=None, workspace_elems=1 
     (dict(heads=0), bp.BP_EINVAL), (dict(kv_heads=0), bp.BP_EINVAL), (dict(kv_heads=3), bp.BP_EINVAL),
     (dict(kv_heads=16), bp.BP_EINVAL), (dict(head_dim=0), bp.BP_EINVAL), (dict(head_dim=513), bp.BP_ESHAPE),
     (dict(tokens=1 << 24), bp.BP_ESHAPE), (dict(heads=16384, kv_heads=2), bp.BP_ESHAPE), (dict(scale=-1.0), bp.BP_EINVAL),
-    (dict(scale=float("nan")), bp.BP_EINVAL), (dict(scale=float("inf")), bp.BP_EINVAL), (dict(ld_q=511), bp.BP_EINVAL),
+    (dict(tokens=(1 << 24) - 1, heads=128), bp.BP_ESHAPE), (dict(scale=float("nan")), bp.BP_EINVAL), (dict(scale=float("inf")), bp.BP_EINVAL), (dict(ld_q=511), bp.BP_EINVAL),
     (dict(ld_k=127), bp.BP_EINVAL), (dict(ld_v=-8), bp.BP_EINVAL), (dict(ld_ctx=1 << 24), bp.BP_ESHAPE)])
 def test_layouts_refused(change, code):
     layout = bp.bp_packed(**{**GOOD, **change})
