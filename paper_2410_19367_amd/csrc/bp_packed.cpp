@@ -173,11 +173,12 @@ int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relp
     a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv;
     a.delta = workspace;
     a.table_part = dtable ? workspace + bp::delta_floats(a) : nullptr;
+    a.dtable = dtable;
+    a.overwrite = overwrite != 0;
     a.dkv_part = workspace + bp::needed_floats(a);
     a.splits = bp::split_heads(a, bp::cu_count());
     if (workspace_elems < bp::needed_floats(a) + bp::part_floats(a, a.splits)) a.splits = 1;
-    hipError_t e = bp::launch(dtype, a, true, (hipStream_t)stream);
-    if (e == hipSuccess && dtable) e = bp::launch_packed_table_grad(a, dtable, overwrite, (hipStream_t)stream);
+    const hipError_t e = bp::launch(dtype, a, true, (hipStream_t)stream);
     if (e != hipSuccess) return fail(BP_EHIP, "packed attention backward: %s", hipGetErrorString(e));
     return BP_OK;
 }

@@ -38,6 +38,8 @@ struct PackedArgs {
     void* dq; void* dk; void* dv;
     float* delta;                           // [heads, T]
     float* table_part;                      // [tiles of kPackedTile rows][heads][buckets], or null: no gradient of the table
+    float* dtable;                          // [buckets, heads]: (+)= the sums of the partials
+    int overwrite;
     int splits;                             // parts of the heads of a key / value head whose dK, dV are summed apart
     float* dkv_part;                        // splits > 1: [splits][T][kv_heads][dK, dV][d]
     RelPos rel;
@@ -61,8 +63,6 @@ hipError_t launch_packed_bwd_rows(int dtype, const PackedArgs& a, hipStream_t s)
 // on the matrix cores: head widths that are multiples of 8 up to 128, 16-byte rows
 hipError_t launch_packed_bf16(const PackedArgs& a, bool back, hipStream_t s);
 hipError_t launch_packed_f32(const PackedArgs& a, bool back, hipStream_t s);
-// dtable (+)= the partials, in a fixed order
-hipError_t launch_packed_table_grad(const PackedArgs& a, float* dtable, int overwrite, hipStream_t s);
 
 #ifdef __HIPCC__
 // Rows lo .. hi - 1 of the sequence that row t lies in; false: in none.  Whatever the starts hold, the rows named are
@@ -88,6 +88,24 @@ __device__ __forceinline__ int packed_bucket(const RelPos& r, const int* start, 
         if (start[m] <= dist) s = m; else e = m;
     }
     return s + (!causal && offset > 0 ? r.n : 0);
+}
+
+// dtable of a head (+)= its partials, by 256 threads in a fixed order: each takes every (256 / buckets)-th of a bucket, then
+// these are added
+__device__ __forceinline__ void sum_table_part(const PackedArgs& a, int head, float* sums) {
+    const int buckets = a.rel.buckets, per = 256 / buckets, b = threadIdx.x % buckets, first = threadIdx.x / buckets;
+    const int tiles = (a.T + kPackedTile - 1) / kPackedTile;
+    float s = 0.f;
+    if (first < per) {
+#pragma unroll 8
+        for (int i = first; i < tiles; i += per) s += a.table_part[((size_t)i * a.heads + head) * buckets + b];
+    }
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (first) return;
+    for (int i = 1; i < per; ++i) s += sums[i * buckets + b];
+    float* out = a.dtable + (size_t)b * a.heads + head;
+    *out = a.overwrite ? s : *out + s;
 }
 #endif
 

@@ -40,6 +40,12 @@ __device__ __forceinline__ int lane_of(unsigned thread) {
     return lane;
 }
 
+// Kernel arguments are cold at every launch: named at the top they are loaded together, with one wait.
+__device__ __forceinline__ void packed_args_now(const PackedArgs& a) {
+    asm volatile("" ::"s"(a.T), "s"(a.n_seq), "s"(a.heads), "s"(a.kv_heads), "s"(a.d), "s"(a.causal), "s"(a.starts), "s"(a.scale),
+                 "s"(a.ld_q), "s"(a.ld_k), "s"(a.ld_v), "s"(a.ld_o), "s"(a.q), "s"(a.k), "s"(a.v));
+}
+
 // ---- what a row sees
 
 // Ranges of the sequences that rows first + lane + 64 r lie in (lo < 0: none), the same rows in every wave of a block.
@@ -244,12 +250,17 @@ __device__ __forceinline__ float sum_by_offset(float* skew, const f32x16& x, int
     return sum;
 }
 
-// step(i, slot) for i < n, i in stage i % 2: with the stage a constant, its LDS offset is part of the instructions
-template <class S>
-__device__ __forceinline__ void two_by_two(int n, S step) {
-    for (int i = 0; i < n; i += 2) {
-        step(i, std::integral_constant<int, 0>{});
-        if (i + 1 < n) step(i + 1, std::integral_constant<int, 1>{});
+// step(i, i % 2) for i < n.  TWO: two steps a turn, so that the stage is a constant and its LDS offset part of the
+// instructions (2 - 5 % of the time at width 128; where registers are short already, it costs more)
+template <bool TWO, class S>
+__device__ __forceinline__ void each_step(int n, S step) {
+    if constexpr (TWO) {
+        for (int i = 0; i < n; i += 2) {
+            step(i, 0);
+            if (i + 1 < n) step(i + 1, 1);
+        }
+    } else {
+        for (int i = 0; i < n; ++i) step(i, i & 1);
     }
 }
 
@@ -352,6 +363,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     constexpr int HP = WIDE ? WIDE : 1, QB = WIDE ? 128 / HP : 64, NH = WIDE ? 2 : 1;
     constexpr int NW = 4, DT = P::DT, TILE = P::TILE, STAGE = 2 * TILE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    packed_args_now(a);
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -390,8 +402,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         m = -INFINITY;
         lsum = 0.f;
         request(0);
-        auto step = [&](int t, auto odd) __attribute__((always_inline)) {
-            constexpr int slot = decltype(odd)::value;
+        auto step = [&](int t, int slot) __attribute__((always_inline)) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (t + 1 < nt) request(t + 1);
@@ -471,7 +482,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                     P::contract(sv, 32 * (kh + u), lane, s[u], ot);
             }
         };
-        two_by_two(nt, step);
+        each_step<true>(nt, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(ot))) walk(std::true_type{});
@@ -534,6 +545,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     constexpr int HP = PAIR ? 2 : 1, QB = 64, NH = PAIR ? 2 : 1;
     constexpr int NW = 4, DT = P::DT, TILE = P::TILE, STAGE = 2 * TILE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    packed_args_now(a);
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -611,8 +623,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             for (int i = lane; i < 8 * kSkewPitch; i += 64) skew[i] = 0.f;
         }
         request(0);
-        auto step = [&](int t, auto odd) __attribute__((always_inline)) {
-            constexpr int slot = decltype(odd)::value;
+        auto step = [&](int t, int slot) __attribute__((always_inline)) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (t + 1 < nt) request(t + 1);
@@ -675,7 +686,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 else P::contract(sk, 32 * kh, lane, dp, dq);
             }
         };
-        two_by_two(nt, step);
+        each_step<true>(nt, step);
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!PAIR) {          // two waves have half the keys of a row each
@@ -742,6 +753,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     constexpr int STAGE = 2 * TILE + 512 + (BIAS ? kMaxBuckets * 4 : 0);       // Q, dO, -lse[64], -delta[64], the head's values
     constexpr int KL = P::kKeysInLds ? P::kKeysInLds - BIAS : 0;        // (two blocks of a CU share 160 KB)
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    packed_args_now(a);
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -814,8 +826,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
         float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1), win1 = fetch_win(g1);
         request(0, 0, smem);
         put(st0, tab0, win0, 0);
-        auto step = [&](int i, auto odd) __attribute__((always_inline)) {
-            constexpr int slot = decltype(odd)::value;
+        auto step = [&](int i, int slot) __attribute__((always_inline)) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (i + 1 < steps) {
@@ -879,7 +890,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
                 P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
             }
         };
-        two_by_two(steps, step);
+        each_step<!(BIAS && DT >= 3)>(steps, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && (any_nan<DT>(dk) || any_nan<DT>(dv)))) walk(std::true_type{});
@@ -922,11 +933,21 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
         }
 }
 
-// dK and dV from the parts' sums, four columns of a row to a thread
+// What is left to sum after dK/dV, in one launch: blocks below a.heads the partials of the table's gradient, if it is wanted,
+// the others dK and dV from the parts' sums, four columns of a row to a thread.
 template <class P>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
+    __shared__ float sums[256];
+    int block = blockIdx.x;
+    if (a.table_part) {
+        if (block < a.heads) {
+            sum_table_part(a, block, sums);
+            return;
+        }
+        block -= a.heads;
+    }
     const int per = a.kv_heads * 2 * a.d / 4;           // threads a row
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t i = (size_t)block * 256 + threadIdx.x;
     const int row = (int)(i / per), c = (int)(i - (size_t)row * per) * 4, kvh = c / (2 * a.d), col = c - kvh * 2 * a.d;
     if (row >= min(a.starts[a.n_seq], a.T) || row < a.starts[0]) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -980,10 +1001,9 @@ static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
     const hipError_t e = allow_lds(packed_dkv_kernel<P, BIAS>, smem, set);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((packed_dkv_kernel<P, BIAS>), dim3(packed_tiles(a.T) * a.kv_heads * a.splits), dim3(256), smem, s, a);
-    if (a.splits > 1) {
-        const size_t threads = (size_t)a.T * (a.kv_heads * 2 * a.d / 4);
-        hipLaunchKernelGGL((packed_join_kernel<P>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
-    }
+    const size_t threads = a.splits > 1 ? (size_t)a.T * (a.kv_heads * 2 * a.d / 4) : 0;
+    const unsigned blocks = (unsigned)((threads + 255) / 256) + (a.table_part ? a.heads : 0);
+    if (blocks) hipLaunchKernelGGL((packed_join_kernel<P>), dim3(blocks), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -195,22 +195,9 @@ __global__ __launch_bounds__(CHUNK) void packed_dkv_rows_kernel(PackedArgs a) {
     }
 }
 
-// dtable[b][head] (+)= sum over the partials: a thread takes every (1024 / buckets)-th of a bucket, then these are added
-__global__ __launch_bounds__(1024) void packed_table_grad_kernel(const float* part, int tiles, int heads, int buckets,
-                                                                 float* dtable, int overwrite) {
-    __shared__ float sums[1024];
-    const int head = blockIdx.x, per = 1024 / buckets, b = threadIdx.x % buckets, first = threadIdx.x / buckets;
-    float s = 0.f;
-    if (first < per) {
-#pragma unroll 4
-        for (int i = first; i < tiles; i += per) s += part[((size_t)i * heads + head) * buckets + b];
-    }
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (first) return;
-    for (int i = 1; i < per; ++i) s += sums[i * buckets + b];
-    float* out = dtable + (size_t)b * heads + head;
-    *out = overwrite ? s : *out + s;
+__global__ __launch_bounds__(256) void packed_table_grad_kernel(PackedArgs a) {
+    __shared__ float sums[256];
+    sum_table_part(a, blockIdx.x, sums);
 }
 
 template <typename T>
@@ -220,6 +207,7 @@ static hipError_t bwd_rows(const PackedArgs& a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((packed_dkv_rows_kernel<T>), dim3(a.T, a.kv_heads), dim3(CHUNK), 0, s, a);
+    if (a.table_part) hipLaunchKernelGGL(packed_table_grad_kernel, dim3(a.heads), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -230,11 +218,6 @@ hipError_t launch_packed_fwd_rows(int dtype, const PackedArgs& a, hipStream_t s)
 }
 hipError_t launch_packed_bwd_rows(int dtype, const PackedArgs& a, hipStream_t s) {
     return dtype ? bwd_rows<bf16_t>(a, s) : bwd_rows<float>(a, s);
-}
-hipError_t launch_packed_table_grad(const PackedArgs& a, float* dtable, int overwrite, hipStream_t s) {
-    hipLaunchKernelGGL(packed_table_grad_kernel, dim3(a.heads), dim3(1024), 0, s, a.table_part, packed_tiles(a.T), a.heads,
-                       a.rel.buckets, dtable, overwrite);
-    return hipGetLastError();
 }
 
 }  // namespace bp
