@@ -686,7 +686,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 else P::contract(sk, 32 * kh, lane, dp, dq);
             }
         };
-        each_step<true>(nt, step);
+        each_step<!BIAS || DT == 4>(nt, step);
         if constexpr (walk == DELTA) {
             delta = halves_sum(pdp);
             if constexpr (!PAIR) {          // two waves have half the keys of a row each
@@ -750,7 +750,7 @@ template <class P, bool BIAS>
 __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedArgs a) {
     typedef typename P::elem elem;
     constexpr int NW = 4, DT = P::DT, KB = 64, TILE = P::TILE;
-    constexpr int STAGE = 2 * TILE + 512 + (BIAS ? kMaxBuckets * 4 : 0);       // Q, dO, -lse[64], -delta[64], the head's values
+    constexpr int STAGE = 2 * TILE + 512;               // Q, dO, -lse[64], -delta[64]
     constexpr int KL = P::kKeysInLds ? P::kKeysInLds - BIAS : 0;        // (two blocks of a CU share 160 KB)
     extern __shared__ __attribute__((aligned(16))) char smem[];
     packed_args_now(a);
@@ -771,12 +771,12 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     const int t0 = x.blk_lo >> 6, nt = ((x.blk_hi + 63) >> 6) - t0;
     const float c = a.scale * P::kUnit;
     RelLds rel{};
-    float* wins = nullptr;                  // values by offset, of the heads of even and of odd steps
+    float* values = nullptr;                // by bucket and by offset, of the heads of even and of odd number
     if constexpr (BIAS) {
         int* start = (int*)(smem + 2 * STAGE);
         for (int i = threadIdx.x; i < a.rel.n; i += 256) start[i] = a.rel.start[i];
-        wins = (float*)(start + kMaxBuckets);
-        rel = {start, nullptr, nullptr, wins + 2 * kWindow + wave * 64};
+        values = (float*)(start + kMaxBuckets);
+        rel = {start, nullptr, nullptr, values + 2 * kRelHead + wave * 64};
     }
     int my_bucket = 0;                      // of this thread's place in the window
     if constexpr (BIAS) my_bucket = fast_bucket(a.rel, a.rel.start, a.causal, (int)threadIdx.x - window_base(a.causal));
@@ -784,10 +784,10 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     TileLoader<P, NW> lq, lo;
     lq.init(wave, lane, a.ld_q, a.d);
     lo.init(wave, lane, a.ld_o, a.d);
-    char* keys = smem + 2 * STAGE + (BIAS ? (kMaxBuckets + 2 * kWindow + 4 * 64) * 4 : 0) + kg * KL * 1024;
+    char* keys = smem + 2 * STAGE + (BIAS ? rel_lds<4, 2>() : 0) + kg * KL * 1024;
     if constexpr (KL > 0)
         if (qh == 0) P::template put_rows<KL>(kf, keys, lane);
-    // Step i takes tile t0 + i % nt of head head0 + i / nt.  Statistics (waves 0 and 1) and the head's values go through
+    // Step i takes tile t0 + i % nt of head head0 + i / nt.  Statistics (waves 0 and 1) and a head's values go through
     // registers, where they get the sign and the base that the exponential and the accumulators want; they are fetched two
     // steps ahead, so that nothing waits for them but the wait at the top of a step.
     const int steps = nt * G;
@@ -798,15 +798,17 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
         const int row = min(max((t0 + t) * 64 + lane, x.blk_lo), x.blk_hi - 1);
         return wave < 2 && g < G ? stat[(size_t)(head0 + g) * a.T + row] : 0.f;
     };
+    auto put_stat = [&](float v, char* stage) {
+        if (wave < 2) ((float*)(stage + 2 * TILE))[wave * 64 + lane] = v * stat_factor;
+    };
     auto fetch_tab = [&](int g) {
         return BIAS && g < G && threadIdx.x < a.rel.buckets ? a.rel.table[(size_t)threadIdx.x * a.heads + head0 + g] : 0.f;
     };
     auto fetch_win = [&](int g) { return BIAS && g < G ? a.rel.table[(size_t)my_bucket * a.heads + head0 + g] : 0.f; };
-    auto put = [&](float st, float tab, float win, int step) {
-        char* stage = smem + (step & 1) * STAGE;
-        if (wave < 2) ((float*)(stage + 2 * TILE))[wave * 64 + lane] = st * stat_factor;
-        if (BIAS && threadIdx.x < a.rel.buckets) ((float*)(stage + 2 * TILE + 512))[threadIdx.x] = tab * P::kUnit;
-        if (BIAS) wins[(step & 1) * kWindow + threadIdx.x] = win * P::kUnit;
+    auto put_values = [&](float tab, float win, int g) {
+        float* to = values + (g & 1) * kRelHead;
+        if (threadIdx.x < a.rel.buckets) to[threadIdx.x] = tab * P::kUnit;
+        to[kMaxBuckets + threadIdx.x] = win * P::kUnit;
     };
     auto request = [&](int g, int t, char* stage) {
         const int r0 = (t0 + t) * 64, col = (head0 + g) * a.d;
@@ -820,32 +822,37 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
         const int lane = lane_of(threadIdx.x), h = lane >> 5;
         clear<DT>(dk);
         clear<DT>(dv);
-        int t = 0, g1 = 0, t1 = 0, g2 = 0, t2 = 0;  // this step's tile; the next step's; the one after it
-        const float st0 = fetch_stat(0, 0), tab0 = fetch_tab(0), win0 = fetch_win(0);
+        int g = 0, t = 0, g1 = 0, t1 = 0, g2 = 0, t2 = 0;       // this step's head and tile; the next step's; those after it
         advance(g1, t1);
-        float st1 = fetch_stat(g1, t1), tab1 = fetch_tab(g1), win1 = fetch_win(g1);
+        const float st0 = fetch_stat(0, 0);
+        float st1 = fetch_stat(g1, t1), tab1 = 0.f, win1 = 0.f;
+        if constexpr (BIAS) {
+            put_values(fetch_tab(0), fetch_win(0), 0);
+            if (t1 == 0) { tab1 = fetch_tab(g1); win1 = fetch_win(g1); }
+        }
         request(0, 0, smem);
-        put(st0, tab0, win0, 0);
+        put_stat(st0, smem);
         auto step = [&](int i, int slot) __attribute__((always_inline)) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
             if (i + 1 < steps) {
-                put(st1, tab1, win1, i + 1);
+                put_stat(st1, smem + (1 - slot) * STAGE);
+                // (the values that a head's first step replaces are those of the last but one)
+                if (BIAS && t1 == 0) put_values(tab1, win1, g1);
                 request(g1, t1, smem + (1 - slot) * STAGE);
                 g2 = g1; t2 = t1;
                 advance(g2, t2);
                 st1 = fetch_stat(g2, t2);
-                tab1 = fetch_tab(g2);
-                win1 = fetch_win(g2);
+                if (BIAS && t2 == 0) { tab1 = fetch_tab(g2); win1 = fetch_win(g2); }
             }
             const char* sq = smem + slot * STAGE;
             const char* sdo = sq + TILE;
             const int q0 = (t0 + t) * 64;
-            t = t1; g1 = g2; t1 = t2;
             if constexpr (BIAS) {
-                rel.tab = (const float*)(sq + 2 * TILE + 512);
-                rel.win = wins + slot * kWindow;
+                rel.tab = values + (g & 1) * kRelHead;
+                rel.win = rel.tab + kMaxBuckets;
             }
+            g = g1; t = t1; g1 = g2; t1 = t2;
             const int qw = q0 + 32 * qh;
             const float* nlse = (const float*)(sq + 2 * TILE) + 32 * qh;
             const float* ndlt = nlse + 64;
@@ -890,7 +897,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
                 P::contract2(sdo, sq, 32 * qh, lane, s, dp, dv, dk);
             }
         };
-        each_step<!(BIAS && DT >= 3)>(steps, step);
+        each_step<!BIAS>(steps, step);
     };
     walk(std::false_type{});
     if (__syncthreads_or(x.hi > x.lo && (any_nan<DT>(dk) || any_nan<DT>(dv)))) walk(std::true_type{});
@@ -994,7 +1001,7 @@ static hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
 }
 template <class P, bool BIAS>
 static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
-    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? kMaxBuckets * 12 + (2 * kWindow + 4 * 64) * sizeof(float) : 0) +
+    constexpr size_t stages = (size_t)2 * (2 * P::TILE + 512) + (BIAS ? rel_lds<4, 2>() : 0) +
                               (P::kKeysInLds ? (P::kKeysInLds - BIAS) * 2 * 1024 : 0);
     constexpr size_t smem = std::max(stages, (size_t)2 * 2 * P::DT * 16 * 64 * sizeof(float));
     static std::atomic<uint64_t> set{0};
