@@ -45,13 +45,16 @@ struct PackedArgs {
     RelPos rel;
 };
 
-// Parts into which the heads that share a key / value head are divided for dK and dV.  One where the blocks of 64 keys fill
-// the chip by themselves: each has G times a dQ block's work, and few of them leave most of the chip idle.
+// Parts into which the heads that share a key / value head are divided for dK and dV: as many as make `blocks` blocks of 64
+// keys for a CU.  Few blocks, each with the work of a group of heads, leave most of the chip idle; the parts' sums go through
+// memory, which long sequences pay and short ones do not.  Whole backward with 1 / 2 / 4 blocks a CU, us, from 256 of one
+// part on: one sequence of 8192, 8 heads of 128 on 2 905 / 624 / 508; 2048 tokens, 32 on 8 252 / 187 / 168; 4 sequences
+// of 512 92.7 / 89.3 / 96.8; from 512, 16 of 256 tokens 100 / 99 / 125; 200 of 1 to 40, 32 of 96 on 4 73 / 81 / 92.
 inline int split_heads(const PackedArgs& a, int cus) {
-    const int G = a.heads / a.kv_heads;
-    const long blocks = (long)((a.T + kPackedTile - 1) / kPackedTile) * a.kv_heads;
+    const int G = a.heads / a.kv_heads, mean = a.T / a.n_seq, blocks = mean >= 1024 ? 4 : mean >= 128 ? 2 : 1;
+    const long one = (long)((a.T + kPackedTile - 1) / kPackedTile) * a.kv_heads;
     int s = 1;
-    while (s < G && (G % s || blocks * s < 4L * cus)) ++s;
+    while (s < G && (G % s || one * s < (long)blocks * cus)) ++s;
     return s;
 }
 
