@@ -13,9 +13,10 @@
 //
 // Values that are not finite.  A masked pair has p = 0, but zero times NaN is not zero in the second product.  Only NaN
 // comes of that, so a block that ends with NaN in a result takes its tiles once more, with the second products done row by
-// row on the vector units and the masked pairs left out (some fifteen times the time of the first walk).  A block without
-// NaN pays one look at its results; the second walk is code of its own, without a branch to the matrix cores in it, which
-// kept all accumulators twice (registers of the forward at width 64: 112 alone, 118 with this walk, 162 with the branch).
+// row on the vector units and the masked pairs left out (every value NaN: forward 9 - 32 times as long, backward 17 - 35).
+// A block without NaN pays one look at its results; the second walk is code of its own, without a branch to the matrix
+// cores in it, which kept all accumulators twice (registers of the forward at width 64: 112 alone, 118 with this walk, 162
+// with the branch).
 //
 // Key / value heads that several query heads share: blocks of query heads of the same one run on the same XCD (position
 // modulo kv_heads first), and a dK/dV block walks its heads one after the other, so shared gradients are sums in
