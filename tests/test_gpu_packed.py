@@ -220,6 +220,38 @@ def test_packed_wide_blocks_what_is_not_finite(lens, H, Hk, d, causal):
     assert np.isnan(got["ctx"][at, H - G:, 1]).all()
 
 
+# More starts than a wave loads at once, two and three levels of them; hundreds of empty sequences inside one block of rows
+@pytest.mark.parametrize("lens", [[0] * 3000 + [1, 2, 0, 0, 0] * 700 + [0] * 900, [3] + [0] * 500 + [70, 0, 1] + [0] * 130 + [90] + [0] * 64,
+                                  [0] * 63 + [100], [0] * 64 + [100], [1] * 63 + [40], [5] * 64 + [0] * 4100 + [61]])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_many_sequences(lens, causal):
+    c = Call(lens, 2, 1, 64, causal, "bf16", front=2, back=1, buckets=8, far=30)
+    c.check(c.run())
+
+
+# Rows farther apart than their heads, one key / value head for all, blocks of both kinds
+@pytest.mark.parametrize("lens,H,Hk,d,gap", [([200, 31, 90], 64, 1, 64, 8), ([200, 31, 90], 24, 1, 128, 16), ([70, 300], 6, 6, 40, 24),
+                                             ([150] * 20, 32, 2, 96, 8)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_row_pitch_and_one_kv_head(lens, H, Hk, d, gap, dtype):
+    if dtype == "f32":
+        lens = lens[:3]
+    c = Call(lens, H, Hk, d, True, dtype, back=4, gap=gap, buckets=16, far=50)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_table_gradient_next_to_what_is_not_finite(dtype):
+    """The table's gradient takes nothing from masked pairs or from rows of no sequence: a NaN behind the last token that
+    has a gradient, and NaN in every padding row."""
+    c = Call([50, 90, 40], 2, 1, 64, True, dtype, front=9, back=30, buckets=16, far=40)
+    r = c.reference()
+    for x in (c.q, c.k, c.v, c.g):
+        x[:9] = np.nan
+        x[c.starts[-1]:] = np.nan
+    c.check(c.run(), r)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_packed_least_workspace(dtype):
     """Without room for the sums of parts, shared heads are summed in one block."""
