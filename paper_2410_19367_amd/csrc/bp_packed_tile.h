@@ -96,7 +96,9 @@ struct Ranges {
     int lo, hi;                             // of this lane's row; lo == hi: none
     int inner_lo, inner_hi;                 // what all rows of the wave see; inner_hi 0: it has none
     int blk_lo, blk_hi;                     // outermost ends of the block's; blk_hi 0: none
+    int short_lo, short_hi;                 // and of its ranges of up to kShort rows; short_hi 0: none (64 rows only)
 };
+constexpr int kShort = 256;
 // rows: 64 or 128 of a block; mine: this lane's row within it.  by_key: what a key is seen by, else what a query sees
 template <int QB>
 __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, int mine, int lane, bool by_key) {
@@ -104,7 +106,7 @@ __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, i
     int lo[R], hi[R];
     seq_ranges<R>(a.starts, a.n_seq, a.T, first, lane, lo, hi);
     Ranges x;
-    x.blk_lo = x.blk_hi = 0;
+    x.blk_lo = x.blk_hi = x.short_lo = x.short_hi = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = first + lane + 64 * r;
@@ -115,6 +117,11 @@ __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, i
         if (valid) {
             if (!x.blk_hi) x.blk_lo = __builtin_amdgcn_readlane(lo[r], __builtin_ctzll(valid));
             x.blk_hi = __builtin_amdgcn_readlane(hi[r], 63 - __builtin_clzll(valid));
+        }
+        const uint64_t few = R == 1 ? __builtin_amdgcn_ballot_w64(ok && hi[r] - lo[r] <= kShort) : 0;
+        if (few) {
+            x.short_lo = __builtin_amdgcn_readlane(lo[r], __builtin_ctzll(few));
+            x.short_hi = __builtin_amdgcn_readlane(hi[r], 63 - __builtin_clzll(few));
         }
     }
     x.lo = __shfl(lo[0], mine & 63, 64);
@@ -530,13 +537,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
 // delta = dO . ctx, or the sum of P dP over a first walk of the keys where the rounding of ctx to bf16 would be felt:
 //   the table's gradient is wanted: the last buckets' sums are small differences of many pairs (half a percent of them came
 //     from the rounding at 2048 tokens);
-//   a block has few keys, so that delta is not small beside dP: up to kShort tiles (relative error of dQ over sequences of
-//     1 to 40 tokens 2.8e-3 before, of which 1.7e-3 is the rounding of dQ itself).
+//   a row has few keys, so that delta is not small beside dP: up to kShort; the walk is over the tiles of such rows only
+//     (relative error of dQ over sequences of 1 to 40 tokens 2.8e-3 before, now 2.4e-3; 1.7e-3 is the rounding of dQ itself
+//     and as much that of dS).
 //
 // The table's gradient: a piece of one bucket adds dS to a register; others are summed by offset (sum_by_offset).  Sums by
 // offset become sums by bucket with a segmented sum over the lanes: of the window once, at the end; of a piece outside at once.
 // =====================================================================================
-constexpr int kShort = 4;
 template <int NW> constexpr size_t table_lds() { return (size_t)NW * (8 * kSkewPitch + kMaxBuckets + kWindow) * sizeof(float); }
 
 template <class P, bool PAIR, bool BIAS>
@@ -596,9 +603,9 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
     TileLoader<P, NW> lk, lv;
     lk.init(wave, lane, a.ld_k, a.d);
     lv.init(wave, lane, a.ld_v, a.d);
-    auto request = [&](int t) {
-        char* st = smem + (t & 1) * STAGE;
-        const int r0 = (t0 + t) * 64;
+    auto request = [&](int tile, int slot) {
+        char* st = smem + slot * STAGE;
+        const int r0 = tile * 64;
         lk.issue(kbase + (size_t)r0 * a.ld_k, a.ld_k, a.d, x.blk_lo - r0, x.blk_hi - r0, st, wave);
         lv.issue(vbase + (size_t)r0 * a.ld_v, a.ld_v, a.d, x.blk_lo - r0, x.blk_hi - r0, st + TILE, wave);
     };
@@ -623,16 +630,18 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             for (int i = lane; i < kWindow; i += 64) near[i] = 0.f;
             for (int i = lane; i < 8 * kSkewPitch; i += 64) skew[i] = 0.f;
         }
-        request(0);
+        const bool all = walk != DELTA || grad;
+        const int first = all ? t0 : x.short_lo >> 6, n = all ? nt : ((x.short_hi + 63) >> 6) - first;
+        request(first, 0);
         auto step = [&](int t, int slot) __attribute__((always_inline)) {
             BP_WAIT_VMCNT(0);
             __syncthreads();
-            if (t + 1 < nt) request(t + 1);
+            if (t + 1 < n) request(first + t + 1, 1 - slot);
             const char* sk = smem + slot * STAGE;
             const char* sv = sk + TILE;
 #pragma unroll
             for (int kh = kh0; kh < kh0 + NH; ++kh) {
-                const int kw = (t0 + t) * 64 + 32 * kh;
+                const int kw = (first + t) * 64 + 32 * kh;
                 f32x16 s, dp;
                 const float d0 = walk == DELTA ? 0.f : -delta;
 #pragma unroll
@@ -687,15 +696,16 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 else P::contract(sk, 32 * kh, lane, dp, dq);
             }
         };
-        each_step<!BIAS || DT == 4>(nt, step);
+        each_step<!BIAS || DT == 4>(n, step);
         if constexpr (walk == DELTA) {
-            delta = halves_sum(pdp);
+            float sum = halves_sum(pdp);
             if constexpr (!PAIR) {          // two waves have half the keys of a row each
                 float* ex = (float*)(smem + 2 * STAGE + (BIAS ? rel_lds<NW, 1>() : 0));      // the place of `skew`
-                ex[wave * 64 + lane] = delta;
+                ex[wave * 64 + lane] = sum;
                 __syncthreads();
-                delta = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
+                sum = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
             }
+            if (all || (x.lo >= x.short_lo && x.hi <= x.short_hi)) delta = sum;        // all of the row's keys were there
             __syncthreads();                // (and the stages are free for the next walk)
         } else if (grad) {
             flush();
@@ -705,7 +715,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         }
     };
     if constexpr (P::kRounds)
-        if (grad || nt <= kShort) walk_keys(std::integral_constant<int, DELTA>{});
+        if (grad || x.short_hi) walk_keys(std::integral_constant<int, DELTA>{});
     walk_keys(std::integral_constant<int, GRAD>{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(dq))) walk_keys(std::integral_constant<int, BY_ROWS>{});
     if (kh0 == 0 && h == 0 && x.hi > x.lo) a.delta[li] = delta;

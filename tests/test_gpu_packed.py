@@ -220,6 +220,18 @@ def test_packed_wide_blocks_what_is_not_finite(lens, H, Hk, d, causal):
     assert np.isnan(got["ctx"][at, H - G:, 1]).all()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_short_sequences_behind_long_ones(causal):
+    """delta of rows with few keys does not come from the rounded ctx, also where their block holds the end of a long
+    sequence: what is left in dQ of these rows are two roundings of equal size, of dS and of dQ itself (their norms add up to
+    sqrt(2) times one), and a tenth for all else."""
+    c = Call([700, 20, 30, 600, 9, 25, 300, 14], 8, 2, 64, causal, "bf16")
+    got, r = c.run(), c.reference()
+    rows = np.concatenate([np.arange(s, e) for s, e in zip(c.starts[:-1], c.starts[1:]) if e - s <= 30])
+    one = np.linalg.norm(si.round_bf16(r["dq"][rows]) - r["dq"][rows])
+    assert np.linalg.norm(got["dq"][rows] - r["dq"][rows]) <= 1.55 * one
+
+
 # More starts than a wave loads at once, two and three levels of them; hundreds of empty sequences inside one block of rows
 @pytest.mark.parametrize("lens", [[0] * 3000 + [1, 2, 0, 0, 0] * 700 + [0] * 900, [3] + [0] * 500 + [70, 0, 1] + [0] * 130 + [90] + [0] * 64,
                                   [0] * 63 + [100], [0] * 64 + [100], [1] * 63 + [40], [5] * 64 + [0] * 4100 + [61]])
