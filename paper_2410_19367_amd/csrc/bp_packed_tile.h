@@ -230,6 +230,16 @@ __device__ __forceinline__ void clear(f32x16 (&x)[DT]) {
         for (int v = 0; v < 16; ++v) x[t][v] = 0.f;
 }
 
+// What a lane has of a piece, in pairs: sums over the pieces of a long row that take these have a sixteenth of the terms, each
+// rounded to the size of the sum.  (16 values one after the other, 5091 tokens without a causal mask: gradient of the bias
+// table off by 8.6e-7, now 7.7e-7, at the same speed.)
+__device__ __forceinline__ float sum_of(const f32x16& x) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (x[4 * i] + x[4 * i + 1]) + (x[4 * i + 2] + x[4 * i + 3]);
+    return (y[0] + y[1]) + (y[2] + y[3]);
+}
+
 // a wave's own LDS: what its lanes have written is there for all of them
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -679,8 +689,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 for (int v = 0; v < 16; ++v)                // dS^T, or P dP
                     dp[v] = (BIAS && walk != DELTA ? dp[v] - delta : dp[v]) * P::expo(__builtin_fmaf(s[v], f, o));
                 if constexpr (walk == DELTA) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) pdp += dp[v];
+                    pdp += sum_of(dp);
                     continue;
                 }
                 if constexpr (BIAS) {
@@ -688,8 +697,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                         bucket = __builtin_amdgcn_readfirstlane(bucket);
                         if (bucket != far_bucket) flush();
                         far_bucket = bucket;
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) far += dp[v];
+                        far += sum_of(dp);
                     } else if (grad) {
                         const float sum = sum_by_offset(skew, dp, lane);
                         if (kind == LOOKED_UP) add_by_bucket(sums, bucket, sum, lane);
