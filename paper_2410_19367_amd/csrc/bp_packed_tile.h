@@ -97,6 +97,7 @@ struct Ranges {
     int inner_lo, inner_hi;                 // what all rows of the wave see; inner_hi 0: it has none
     int blk_lo, blk_hi;                     // outermost ends of the block's; blk_hi 0: none
     int short_lo, short_hi;                 // and of its ranges of up to kShort rows; short_hi 0: none (64 rows only)
+    uint64_t alone;                         // a bit for each row of the block: a sequence of one row (64 rows only)
 };
 constexpr int kShort = 256;
 // rows: 64 or 128 of a block; mine: this lane's row within it.  by_key: what a key is seen by, else what a query sees
@@ -107,6 +108,7 @@ __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, i
     seq_ranges<R>(a.starts, a.n_seq, a.T, first, lane, lo, hi);
     Ranges x;
     x.blk_lo = x.blk_hi = x.short_lo = x.short_hi = 0;
+    x.alone = R == 1 ? __builtin_amdgcn_ballot_w64(lo[0] >= 0 && hi[0] - lo[0] == 1) : 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = first + lane + 64 * r;
@@ -585,6 +587,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         delta = halves_sum(P::dot(of, dof));
     }
     const Ranges x = block_ranges<QB>(a, blk * QB, qg * 32 + (lane & 31), lane, false);
+    // Of one key alone dS is 0, not what two roundings of dP and delta leave (but NaN where they are not finite).
+    const bool one = x.hi - x.lo == 1;
+    if (one && kh0 == 0 && h == 0) a.delta[li] = delta;
+    if (one && delta - delta == 0.f) {
+        P::zero(dof);
+        delta = 0.f;
+    }
     const bool grad = BIAS && a.table_part;
     auto put_part = [&](float v) { a.table_part[((size_t)blk * a.heads + head) * a.rel.buckets + threadIdx.x] = v; };
     if (!x.blk_hi) {
@@ -730,7 +739,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
         if (grad || x.short_hi) walk_keys(std::integral_constant<int, DELTA>{});
     walk_keys(std::integral_constant<int, GRAD>{});
     if (__syncthreads_or(x.hi > x.lo && any_nan<DT>(dq))) walk_keys(std::integral_constant<int, BY_ROWS>{});
-    if (kh0 == 0 && h == 0 && x.hi > x.lo) a.delta[li] = delta;
+    if (kh0 == 0 && h == 0 && x.hi > x.lo + 1) a.delta[li] = delta;
 
     __syncthreads();
     if (grad && threadIdx.x < a.rel.buckets) {
@@ -938,6 +947,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     __syncthreads();
     if (qh == 1) return;
     if (x.hi <= x.lo) return;
+    const float scale = (x.alone >> (kg * 32 + (lane & 31))) & 1 ? 0.f : a.scale;       // (dS is 0 there, as in dQ)
     elem* dk_out = (elem*)a.dk + (size_t)k_lane * a.ld_k + kvh * a.d;
     elem* dv_out = (elem*)a.dv + (size_t)k_lane * a.ld_v + kvh * a.d;
     float* sums = a.splits > 1 ? a.dkv_part + (((size_t)part * a.T + k_lane) * a.kv_heads + kvh) * 2 * a.d : nullptr;
@@ -949,7 +959,7 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
             f32x4 k4, v4;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                k4[e] = (dk[t][4 * g + e] + xo[(t * 16 + 4 * g + e) * 64 + lane]) * a.scale;
+                k4[e] = (dk[t][4 * g + e] + xo[(t * 16 + 4 * g + e) * 64 + lane]) * scale;
                 v4[e] = dv[t][4 * g + e] + xo[((DT + t) * 16 + 4 * g + e) * 64 + lane];
             }
             if (col >= a.d) continue;

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(CHUNK) void packed_dq_rows_kernel(PackedArgs a, int
             const int n = min(CHUNK, hi - j0);
             float p = 0.f, dp = 0.f;
             if (tid < n) scores(j0 + tid, p, dp);
-            ds[tid] = tid < n ? p * (dp - delta) : 0.f;
+            ds[tid] = tid < n ? p * (dp - delta) * (hi - lo == 1 ? 0.f : 1.f) : 0.f;    // 0 of one key alone, NaN if it is
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < COLS; ++i) {
@@ -153,6 +153,7 @@ __global__ __launch_bounds__(CHUNK) void packed_dkv_rows_kernel(PackedArgs a) {
     const int t = blockIdx.x, kvh = blockIdx.y, G = a.heads / a.kv_heads, tid = threadIdx.x;
     int lo, hi;
     if (!packed_row_range(a, t, lo, hi)) return;
+    const float scale = hi - lo == 1 ? 0.f : a.scale;       // dS of one key alone is 0
     if (a.causal) lo = t;
     load_starts(a.rel, start);
     for (int c = tid; c < a.d; c += CHUNK) {
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(CHUNK) void packed_dkv_rows_kernel(PackedArgs a) {
     for (int x = 0; x < COLS; ++x) {
         const int c = tid + x * CHUNK;
         if (c >= a.d) break;
-        ((T*)a.dk)[(size_t)t * a.ld_k + kvh * a.d + c] = from_float<T>(dk[x] * a.scale);
+        ((T*)a.dk)[(size_t)t * a.ld_k + kvh * a.d + c] = from_float<T>(dk[x] * scale);
         ((T*)a.dv)[(size_t)t * a.ld_v + kvh * a.d + c] = from_float<T>(dv[x]);
     }
 }

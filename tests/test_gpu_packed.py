@@ -501,3 +501,17 @@ def test_packed_block_of_a_layer():
     r_dqkv = np.concatenate([r[n].reshape(T, -1) for n in ("dq", "dk", "dv")], 1)
     assert hz.rel_err(hz.to_host(dw), x.T @ r_dqkv) < 2e-5
     assert hz.rel_err(hz.to_host(dtable), r["dtable"]) < 2e-5
+
+
+@pytest.mark.parametrize("d,shift", [(64, 0), (128, 0), (40, 1)])
+@pytest.mark.parametrize("causal,buckets", [(True, 0), (False, 0), (True, 16), (False, 16)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_one_key_alone_has_no_gradient_of_its_score(dtype, causal, buckets, d, shift):
+    """The one probability is 1 whatever the score is: dq, dk and the table's gradient are 0, not a rounding's remainder."""
+    c = Call([1, 0, 1, 1] * 30, 4, 2, d, causal, dtype, front=2, back=3, buckets=buckets, far=32, shift=shift)
+    got = c.run()
+    for name in ("dq", "dk"):
+        assert (got[name][2:-3] == 0).all(), name
+    if buckets:
+        assert (got["dtable"] == 0).all()
+    c.check(got)
