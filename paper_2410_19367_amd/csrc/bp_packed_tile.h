@@ -691,12 +691,18 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                     for (int v = 0; v < 16; ++v)
                         if ((unsigned)(kw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {
                             s[v] = -INFINITY;
-                            if (walk != GRAD) dp[v] = 0.f;      // (NaN otherwise, which brings about the last walk)
+                            if (walk == DELTA) dp[v] = 0.f;     // (NaN otherwise, which brings about the last walk)
                         }
                 }
 #pragma unroll
                 for (int v = 0; v < 16; ++v)                // dS^T, or P dP
                     dp[v] = (BIAS && walk != DELTA ? dp[v] - delta : dp[v]) * P::expo(__builtin_fmaf(s[v], f, o));
+                // delta or lse of a row may be NaN: pairs that the row does not see are left out of the sums below by its
+                // own range, also in pieces that other rows see whole, for a row of no sequence
+                if constexpr (BIAS && walk == BY_ROWS)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if ((unsigned)(kw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) dp[v] = 0.f;
                 if constexpr (walk == DELTA) {
                     pdp += sum_of(dp);
                     continue;

@@ -1,0 +1,111 @@
+"""GPU: attention over packed sequences where a row holds what is not finite or sees nothing, against a 64-bit form that takes
+visible pairs only."""
+import numpy as np
+import pytest
+
+from oracle import packed_oracle as po
+from tests.test_gpu_packed import UNIT, Call
+
+pytestmark = pytest.mark.gpu
+
+
+def by_rows(c):
+    """The definition row by row in fp64, in the layout of po.attention: nothing is made of a pair that is not visible, so
+    what is not finite in the result depends on what is not finite in the inputs.  abs_*: sums of absolute terms."""
+    G = c.H // c.Hk
+    shapes = dict(ctx=c.q.shape, lse=(c.H, c.T), dq=c.q.shape, dk=c.k.shape, dv=c.v.shape)
+    r = {p + n: np.zeros(s) for n, s in shapes.items() for p in ("", "abs_")}
+    if c.table is not None:
+        r |= {"dtable": np.zeros(c.table.shape), "abs_dtable": np.zeros(c.table.shape)}
+    bucket = {}
+    z_most = 0.0
+    with np.errstate(all="ignore"):
+        for s0, s1 in zip(c.starts[:-1], c.starts[1:]):
+            for i in range(s0, s1):
+                js = np.arange(s0, i + 1 if c.causal else s1)
+                if c.table is not None:
+                    of = js - i
+                    for o in of:
+                        if o not in bucket:
+                            bucket[o] = po.bucket(c.causal, len(c.table), c.far, int(o))
+                    b = np.array([bucket[o] for o in of])
+                for h in range(c.H):
+                    K, V, g = c.k[js, h // G], c.v[js, h // G], c.g[i, h]
+                    z, zabs = c.scale * (K @ c.q[i, h]), c.scale * (np.abs(K) @ np.abs(c.q[i, h]))
+                    if np.isfinite(zabs).all():
+                        z_most = max(z_most, float(zabs.max()))
+                    if c.table is not None:
+                        z = z + np.where(c.table[b, h] <= -1e30, -np.inf, c.table[b, h])
+                    top = z.max()
+                    e = np.exp(z - top)
+                    p = e / e.sum()
+                    dp, dpa = V @ g, np.abs(V) @ np.abs(g)
+                    ds = p * (dp - (p * dp).sum())
+                    dsa = p * (dpa + (p * dpa).sum())
+                    r["lse"][h, i] = top + np.log(e.sum())
+                    r["ctx"][i, h], r["abs_ctx"][i, h] = p @ V, p @ np.abs(V)
+                    r["dq"][i, h], r["abs_dq"][i, h] = c.scale * (ds @ K), c.scale * (dsa @ np.abs(K))
+                    r["dk"][js, h // G] += c.scale * ds[:, None] * c.q[i, h]
+                    r["abs_dk"][js, h // G] += c.scale * dsa[:, None] * np.abs(c.q[i, h])
+                    r["dv"][js, h // G] += p[:, None] * g
+                    r["abs_dv"][js, h // G] += p[:, None] * np.abs(g)
+                    if c.table is not None:
+                        np.add.at(r["dtable"][:, h], b, ds)
+                        np.add.at(r["abs_dtable"][:, h], b, dsa)
+    r["abs_lse"] = np.abs(r["lse"])
+    r["z"] = z_most
+    return r
+
+
+def check(c, got, r):
+    """Finite where the definition is, within the bounds, and not where it is not (lse of a row that sees nothing is -inf)."""
+    with np.errstate(all="ignore"):
+        tol = po.bounds(r, c.longest, c.d, c.H // c.Hk, UNIT[c.dtype])
+    for name, a in got.items():
+        ref, t = r[name], tol[name] * np.ones_like(r[name])
+        if name != "dtable":
+            rows = slice(c.starts[0], c.starts[-1])
+            a, ref, t = (x[:, rows] if name == "lse" else x[rows] for x in (a, ref, t))
+        if name in ("dq", "dk") and c.dtype == "bf16":
+            t = 2.0 * t                         # ctx's rounding in delta, as in Call.check
+        fine = np.isfinite(ref)
+        assert not np.isfinite(a[~fine]).any(), (name, "finite where the definition is not")
+        assert np.isfinite(a[fine]).all(), (name, np.argwhere(fine & ~np.isfinite(a))[:8].tolist())
+        if fine.any():
+            off = np.abs(a[fine] - ref[fine]) / (t[fine] + 1e-30)
+            assert off.max() <= 1.0, (name, float(off.max()))
+
+
+# head width and shift of the pointers: the matrix-core kernels and the row kernels
+KERNELS = [(64, 0), (128, 0), (64, 1)]
+
+
+@pytest.mark.parametrize("d,shift", KERNELS)
+@pytest.mark.parametrize("lens,causal,at", [([40, 24], True, 50), ([24, 40], True, 20), ([300, 3], True, 301), ([2, 300, 60], True, 30),
+                                            ([40, 24], False, 50), ([300, 3], False, 301)])
+@pytest.mark.parametrize("where", ["q", "g", "k", "v"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_table_gradient_takes_nothing_from_pairs_that_are_not_visible(dtype, where, lens, causal, at, d, shift):
+    """NaN in a row inside a sequence reaches the buckets of the distances that its queries see, in its heads, and no others."""
+    c = Call(lens, 4, 2, d, causal, dtype, front=3, back=5, buckets=16, far=40, shift=shift)
+    getattr(c, where)[c.starts[0] + at, 1, 3] = np.nan
+    for x in (c.q, c.k, c.v, c.g):
+        x[:3] = np.nan
+        x[c.starts[-1]:] = np.nan
+    r = by_rows(c)
+    assert np.isnan(r["dtable"]).any() and np.isfinite(r["dtable"]).any()
+    check(c, c.run(), r)
+
+
+@pytest.mark.parametrize("d,shift", KERNELS)
+@pytest.mark.parametrize("low", [-np.inf])
+@pytest.mark.parametrize("buckets,causal", [([0], True), ([0, 1, 2], True), ([0, 1, 9], False)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_query_that_sees_nothing_is_nan_and_reaches_its_own_keys_only(dtype, buckets, causal, low, d, shift):
+    """Buckets taken out of one head leave the first rows of its sequences (without a mask: sequences of one and two rows)
+    nothing to look at."""
+    c = Call([70, 1, 2, 150, 30], 4, 2, d, causal, dtype, front=2, back=3, buckets=16, far=40, shift=shift)
+    c.table[buckets, 1] = low
+    r = by_rows(c)
+    assert np.isnan(r["ctx"][:, 1]).any() and np.isfinite(r["ctx"][:, [0, 2, 3]]).all()
+    check(c, c.run(), r)
