@@ -460,13 +460,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                     for (int v = 0; v < 16; ++v)
                         if ((unsigned)(kw + 32 * u + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) s[u][v] = -INFINITY;
             }
-            float mx = -INFINITY;
+            float mx = -INFINITY, w[NH];
 #pragma unroll
             for (int u = 0; u < NH; ++u) {
-                float w = s[u][0];
+                w[u] = s[u][0];
 #pragma unroll
-                for (int v = 1; v < 16; ++v) w = fmaxf(w, s[u][v]);
-                mx = fmaxf(mx, BIAS ? __builtin_fmaf(w, f[u], o[u]) : w);
+                for (int v = 1; v < 16; ++v) w[u] = fmaxf(w[u], s[u][v]);
+                mx = fmaxf(mx, BIAS ? __builtin_fmaf(w[u], f[u], o[u]) : w[u]);
             }
             mx = halves_max(mx);
             if (!BIAS) mx *= c;
@@ -484,7 +484,19 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             const float m_use = m == -INFINITY ? 0.f : m;       // nothing but -inf so far: no inf - inf
 #pragma unroll
             for (int u = 0; u < NH; ++u) {
-                const float off = BIAS ? o[u] - m_use : -m_use;
+                float off = -m_use;
+                if constexpr (BIAS) {
+                    off = o[u] - m_use;
+                    // A value beyond some 2^27 rounds the scores away in m, not in s: they join it here, one by one, or the
+                    // exponential of a large score, with nothing subtracted, would be infinite.
+                    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(w[u], f[u], off) > 16.f * P::kBit) != 0) {
+                        asm volatile("");
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) s[u][v] = __builtin_fmaf(s[u][v], f[u], o[u]);
+                        f[u] = 1.f;
+                        off = -m_use;
+                    }
+                }
                 float ps = 0.f;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {

@@ -1,5 +1,5 @@
-"""GPU: attention over packed sequences where a row holds what is not finite or sees nothing, against a 64-bit form that takes
-visible pairs only."""
+"""GPU: attention over packed sequences where a row holds what is not finite or sees nothing, or a bucket of the bias is far
+from every score, against a 64-bit form that takes visible pairs only."""
 import numpy as np
 import pytest
 
@@ -108,4 +108,23 @@ def test_a_query_that_sees_nothing_is_nan_and_reaches_its_own_keys_only(dtype, b
     c.table[buckets, 1] = low
     r = by_rows(c)
     assert np.isnan(r["ctx"][:, 1]).any() and np.isfinite(r["ctx"][:, [0, 2, 3]]).all()
+    check(c, c.run(), r)
+
+
+@pytest.mark.parametrize("d,shift", KERNELS)
+@pytest.mark.parametrize("value", [-1e9, -1e12, -1e20, -3.0e38, 1e12])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bucket_far_from_all_scores(dtype, causal, value, d, shift):
+    """Scores of hundreds, and a bucket whose bias is far below (or above) them: it takes no probability (or all of it, spread
+    evenly where the bias rounds the scores away).  Far pieces, which a row meets first, lie in this bucket."""
+    c = Call([400, 90], 2, 1, d, causal, dtype, back=2, buckets=16, far=40, std=8.0, shift=shift)
+    c.table[[7, 15] if not causal else [15]] = value
+    if value > 0:                               # only that the result is finite and an average of what the bucket holds
+        got = c.run(backward=False)
+        assert np.isfinite(got["ctx"][:c.starts[-1]]).all()
+        assert np.abs(got["ctx"][:c.starts[-1]]).max() <= np.abs(c.v).max() * (1 + 2 ** -7)
+        return
+    r = by_rows(c)
+    assert r["z"] > 300
     check(c, c.run(), r)
