@@ -424,8 +424,10 @@ typedef struct {
 typedef struct {
     int buckets;            /* causal: 2 .. 128; else even, 4 .. 128                                 */
     int max_distance;       /* above e, below 2^24                                                   */
-    const float* table;     /* dev fp32 [buckets, heads]; -inf (or a value next to the type's lowest) */
-                            /* takes a bucket out; a query with nothing else gets NaN                */
+    const float* table;     /* dev fp32 [buckets, heads]; -inf, which all values up to -1e30 count   */
+                            /* as, takes a bucket out; a query with nothing else gets NaN.  lse is   */
+                            /* fp32: where the largest score of a query, with its bias, is z, the    */
+                            /* backward's probabilities are off by some |z| 2^-24 of themselves      */
 } bp_relpos;
 
 /* Bucket of offset = key position - query position (pure CPU); BP_EINVAL for what the fields above do not allow. */

@@ -82,6 +82,10 @@ __device__ __forceinline__ bool packed_row_range(const PackedArgs& a, int t, int
     return lo <= t && t < hi;
 }
 
+// A value of the bias table as the kernels take it.  Next to the type's lowest it is -inf: it has no room for the scores, and
+// -inf is what leaves a query with nothing else NaN in both directions (p from lse would be 1 for each of its keys).
+__device__ __forceinline__ float packed_bias(float value) { return value <= -1e30f ? -INFINITY : value; }
+
 // bucket of an offset (key minus query); with a causal mask only offsets up to 0 occur
 __device__ __forceinline__ int packed_bucket(const RelPos& r, const int* start, int causal, int offset) {
     const int dist = offset < 0 ? -offset : offset;

@@ -350,10 +350,10 @@ __device__ __forceinline__ RelLds rel_init(const PackedArgs& a, char* lds, int h
 #pragma unroll
     for (int u = 0; u < HP; ++u) {
         for (int i = threadIdx.x; i < a.rel.buckets; i += NW * 64)
-            tab[u * kRelHead + i] = a.rel.table[(size_t)i * a.heads + head + u] * P::kUnit;
+            tab[u * kRelHead + i] = packed_bias(a.rel.table[(size_t)i * a.heads + head + u]) * P::kUnit;
         for (int i = threadIdx.x; i < kWindow; i += NW * 64)
             tab[u * kRelHead + kMaxBuckets + i] =
-                a.rel.table[(size_t)fast_bucket(a.rel, a.rel.start, a.causal, i - window_base(a.causal)) * a.heads + head + u] * P::kUnit;
+                packed_bias(a.rel.table[(size_t)fast_bucket(a.rel, a.rel.start, a.causal, i - window_base(a.causal)) * a.heads + head + u]) * P::kUnit;
     }
     tab += hw * kRelHead;
     return {start, tab, tab + kMaxBuckets, (float*)lds + kMaxBuckets + HP * kRelHead + wave * 64};
@@ -857,8 +857,8 @@ __global__ __launch_bounds__(256, P::kDkvBlocks) void packed_dkv_kernel(PackedAr
     auto fetch_win = [&](int g) { return BIAS && g < G ? a.rel.table[(size_t)my_bucket * a.heads + head0 + g] : 0.f; };
     auto put_values = [&](float tab, float win, int g) {
         float* to = values + (g & 1) * kRelHead;
-        if (threadIdx.x < a.rel.buckets) to[threadIdx.x] = tab * P::kUnit;
-        to[kMaxBuckets + threadIdx.x] = win * P::kUnit;
+        if (threadIdx.x < a.rel.buckets) to[threadIdx.x] = packed_bias(tab) * P::kUnit;
+        to[kMaxBuckets + threadIdx.x] = packed_bias(win) * P::kUnit;
     };
     auto request = [&](int g, int t, char* stage) {
         const int r0 = (t0 + t) * 64, col = (head0 + g) * a.d;

@@ -33,7 +33,7 @@ __device__ __forceinline__ void load_starts(const RelPos& r, int* start) {
     for (int i = threadIdx.x; i < r.n; i += CHUNK) start[i] = r.start[i];
 }
 __device__ __forceinline__ float bias_of(const PackedArgs& a, const int* start, int head, int offset) {
-    return a.rel.buckets ? a.rel.table[(size_t)packed_bucket(a.rel, start, a.causal, offset) * a.heads + head] : 0.f;
+    return a.rel.buckets ? packed_bias(a.rel.table[(size_t)packed_bucket(a.rel, start, a.causal, offset) * a.heads + head]) : 0.f;
 }
 
 template <typename T>

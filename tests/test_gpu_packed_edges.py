@@ -98,7 +98,7 @@ def test_table_gradient_takes_nothing_from_pairs_that_are_not_visible(dtype, whe
 
 
 @pytest.mark.parametrize("d,shift", KERNELS)
-@pytest.mark.parametrize("low", [-np.inf])
+@pytest.mark.parametrize("low", [-np.inf, -3.0e38, -1.0e31])
 @pytest.mark.parametrize("buckets,causal", [([0], True), ([0, 1, 2], True), ([0, 1, 9], False)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_query_that_sees_nothing_is_nan_and_reaches_its_own_keys_only(dtype, buckets, causal, low, d, shift):
