@@ -12,6 +12,7 @@ int cu_count();          // compute units of the device
 constexpr int kMaxBuckets = 128;
 constexpr int kPackedMaxHeadDim = 512;
 constexpr int kPackedTile = 64;             // rows that share one partial of the bias table's gradient
+constexpr int kShort = 256;                 // keys up to which delta of a bf16 row is not taken from its rounded ctx
 
 // Buckets of a relative position: `first` of the offsets in front of the query (0), behind it (n; bidirectional only),
 // plus the number of starts at or below the distance, minus one.

@@ -99,7 +99,6 @@ struct Ranges {
     int short_lo, short_hi;                 // and of its ranges of up to kShort rows; short_hi 0: none (64 rows only)
     uint64_t alone;                         // a bit for each row of the block: a sequence of one row (64 rows only)
 };
-constexpr int kShort = 256;
 // rows: 64 or 128 of a block; mine: this lane's row within it.  by_key: what a key is seen by, else what a query sees
 template <int QB>
 __device__ __forceinline__ Ranges block_ranges(const PackedArgs& a, int first, int mine, int lane, bool by_key) {

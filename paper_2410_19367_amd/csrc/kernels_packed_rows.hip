@@ -110,10 +110,13 @@ __global__ __launch_bounds__(CHUNK) void packed_dq_rows_kernel(PackedArgs a, int
             p = __expf(dot<T>(qs, kb + (size_t)j * a.ld_k, a.d) * a.scale + bias_of(a, start, head, j - t) - lse);
             dp = dot<T>(dos, vb + (size_t)j * a.ld_v, a.d);
         };
-        if (a.table_part) {             // delta from the probabilities, without the rounding of ctx
-            part = 0.f;
-            for (int j = lo + tid; j < hi; j += CHUNK) {
-                float p, dp;
+        const bool once = hi - lo <= CHUNK;     // a key to a thread: what it has of its pair serves delta and dQ
+        float p = 0.f, dp = 0.f;
+        if (once && tid < hi - lo) scores(lo + tid, p, dp);
+        // delta from the probabilities where the rounding of ctx would be felt: the table's gradient, rows of few keys
+        if (a.table_part || (sizeof(T) == 2 && hi - lo <= kShort)) {
+            part = once ? p * dp : 0.f;
+            for (int j = lo + tid; !once && j < hi; j += CHUNK) {
                 scores(j, p, dp);
                 part += p * dp;
             }
@@ -123,8 +126,7 @@ __global__ __launch_bounds__(CHUNK) void packed_dq_rows_kernel(PackedArgs a, int
         float acc[COLS] = {};
         for (int j0 = lo; j0 < hi; j0 += CHUNK) {
             const int n = min(CHUNK, hi - j0);
-            float p = 0.f, dp = 0.f;
-            if (tid < n) scores(j0 + tid, p, dp);
+            if (!once && tid < n) scores(j0 + tid, p, dp);
             ds[tid] = tid < n ? p * (dp - delta) * (hi - lo == 1 ? 0.f : 1.f) : 0.f;    // 0 of one key alone, NaN if it is
             __syncthreads();
 #pragma unroll

@@ -1,8 +1,9 @@
-"""GPU: attention over packed sequences where a row holds what is not finite or sees nothing, or a bucket of the bias is far
-from every score, against a 64-bit form that takes visible pairs only."""
+"""GPU: attention over packed sequences where a row holds what is not finite or sees nothing, where a bucket of the bias is far
+from every score, against a 64-bit form that takes visible pairs only; and the precision of the kernels of one row a block."""
 import numpy as np
 import pytest
 
+import synth_inputs as si
 from oracle import packed_oracle as po
 from tests.test_gpu_packed import UNIT, Call
 
@@ -128,3 +129,15 @@ def test_bucket_far_from_all_scores(dtype, causal, value, d, shift):
     r = by_rows(c)
     assert r["z"] > 300
     check(c, c.run(), r)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,shift", [(64, 1), (40, 1), (7, 0), (136, 0)])
+def test_row_kernels_short_sequences(causal, d, shift):
+    """delta of rows with few keys does not come from the rounded ctx in the kernels of one row a block either.  These keep
+    probabilities and score gradients in fp32, so the rounding of dQ and dK itself is all, and a tenth for all else."""
+    c = Call([20, 30, 9, 25, 14, 200], 8, 2, d, causal, "bf16", shift=shift)
+    got, r = c.run(), c.reference()
+    for name in ("dq", "dk"):
+        one = np.linalg.norm(si.round_bf16(r[name]) - r[name])
+        assert np.linalg.norm(got[name] - r[name]) <= 1.1 * one, (name, np.linalg.norm(got[name] - r[name]) / one)
