@@ -2,6 +2,7 @@
 // group of heads.  Any head width, stride and alignment; nothing but the rows that the row's own sequence lets it see
 // is read.  Keys (queries) come in chunks of 256, one to a thread: its scores need the whole of one row, so reads are
 // as wide as an element and the time goes by their latency.  For the calls that the matrix-core kernels do not take.
+// A chunk is summed by itself before it joins the sum of all, which would round each of its terms to its own size.
 #include "bp_packed.h"
 #include "bp_device.h"
 
@@ -66,9 +67,9 @@ __global__ __launch_bounds__(CHUNK) void packed_fwd_rows_kernel(PackedArgs a) {
         for (int i = 0; i < COLS; ++i) {
             const int c = tid + i * CHUNK;
             if (c >= a.d) break;
-            float s = acc[i] * alpha;
+            float s = 0.f;
             for (int x = 0; x < n; ++x) s += p[x] * to_float<T>(vb[(size_t)(j0 + x) * a.ld_v + c]);
-            acc[i] = s;
+            acc[i] = acc[i] * alpha + s;
         }
         __syncthreads();
     }
@@ -133,11 +134,16 @@ __global__ __launch_bounds__(CHUNK) void packed_dq_rows_kernel(PackedArgs a, int
             for (int i = 0; i < COLS; ++i) {
                 const int c = tid + i * CHUNK;
                 if (c >= a.d) break;
-                for (int x = 0; x < n; ++x) acc[i] += ds[x] * to_float<T>(kb[(size_t)(j0 + x) * a.ld_k + c]);
+                float s = 0.f;
+                for (int x = 0; x < n; ++x) s += ds[x] * to_float<T>(kb[(size_t)(j0 + x) * a.ld_k + c]);
+                acc[i] += s;
             }
-            if (a.table_part && tid < a.rel.buckets)
+            if (a.table_part && tid < a.rel.buckets) {
+                float s = 0.f;
                 for (int x = 0; x < n; ++x)
-                    if (packed_bucket(a.rel, start, a.causal, j0 + x - t) == tid) table += ds[x];
+                    if (packed_bucket(a.rel, start, a.causal, j0 + x - t) == tid) s += ds[x];
+                table += s;
+            }
             __syncthreads();
         }
         T* out = (T*)a.dq + (size_t)t * a.ld_q + head * a.d;
@@ -181,10 +187,13 @@ __global__ __launch_bounds__(CHUNK) void packed_dkv_rows_kernel(PackedArgs a) {
             for (int x = 0; x < COLS; ++x) {
                 const int c = tid + x * CHUNK;
                 if (c >= a.d) break;
+                float sv = 0.f, sk = 0.f;
                 for (int y = 0; y < n; ++y) {
-                    dv[x] += ps[y] * to_float<T>(gb[(size_t)(i0 + y) * a.ld_o + c]);
-                    dk[x] += ds[y] * to_float<T>(qb[(size_t)(i0 + y) * a.ld_q + c]);
+                    sv += ps[y] * to_float<T>(gb[(size_t)(i0 + y) * a.ld_o + c]);
+                    sk += ds[y] * to_float<T>(qb[(size_t)(i0 + y) * a.ld_q + c]);
                 }
+                dv[x] += sv;
+                dk[x] += sk;
             }
             __syncthreads();
         }

@@ -141,3 +141,25 @@ def test_row_kernels_short_sequences(causal, d, shift):
     for name in ("dq", "dk"):
         one = np.linalg.norm(si.round_bf16(r[name]) - r[name])
         assert np.linalg.norm(got[name] - r[name]) <= 1.1 * one, (name, np.linalg.norm(got[name] - r[name]) / one)
+
+
+def test_row_kernels_long_sums():
+    """Equal terms by the ten thousand: the sums of a chunk of 256 are joined, not every term added to the whole, whose
+    rounding would have the same sign each time.  A term goes through at most 256 additions of its chunk, those of the chunks
+    of its row (of its 64 rows for the table's gradient) and of its heads, and of the tiles: terms * 2^-24 of the sum of
+    absolute terms bounds their roundings, `share` is what the probabilities are off by (oracle/packed_oracle.py)."""
+    n, H, Hk, d, far = 4000, 4, 1, 7, 40
+    c = Call([n], H, Hk, d, False, "f32", buckets=8, far=far)
+    c.q[:], c.k[:], c.g[:], c.table[:] = 0.05, 0.01, 0.3, 0.0
+    c.v[:] = 0.7 * (1 + (np.arange(n) % 2 == 0)[:, None, None] * 0.01)
+    c.v[::100] = 5.0
+    got, r = c.run(), c.reference()
+    f = 2.0 ** -24
+    chunks = -(-n // 256)
+    share = 2.0 * (d + 16) * f * (1.0 + r["z"])
+    terms = {"ctx": 256 + chunks, "dq": 256 + chunks, "dk": 256 + chunks * H, "dv": 256 + chunks * H,
+             "dtable": 256 + 64 * chunks + 64}
+    for name, t in terms.items():
+        bound = r["abs_" + name] * (share + (t + 2 * d + 64) * f)
+        off = np.max(np.abs(got[name] - r[name]) / (bound + 1e-30))
+        assert off <= 1.0, (name, float(off))
