@@ -52,26 +52,47 @@ class bp_op(C.Structure):
                 ("stage", C.c_int32), ("mb", C.c_int32)]
 
 
+def _kernel_array(name, t, dtype, elems):
+    """Address of what a kernel reads as `elems` values of `dtype` one behind the other: a tensor in device or pinned memory
+    that holds them, or an address, which is taken as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    if str(getattr(t, "dtype", "")) != "torch." + dtype:
+        raise BitPipeError(BP_EINVAL, f"{name} must be a {dtype} tensor, not {getattr(t, 'dtype', type(t).__name__)}")
+    if not t.is_contiguous() or t.numel() < elems:
+        raise BitPipeError(BP_EINVAL, f"{name} must be contiguous with at least {elems} elements, not {tuple(t.shape)}")
+    if not (t.is_cuda or t.is_pinned()):
+        raise BitPipeError(BP_EINVAL, f"{name} must lie in device memory")
+    return t.data_ptr()
+
+
 class bp_packed(C.Structure):
-    """Packed sequences.  `starts`: int32 device tensor (kept alive by this object) or its address."""
+    """Packed sequences.  `starts`: contiguous int32 device tensor of sequences + 1 (kept alive by this object) or its address."""
     _fields_ = [("tokens", C.c_int), ("sequences", C.c_int), ("starts", C.c_void_p), ("heads", C.c_int),
                 ("kv_heads", C.c_int), ("head_dim", C.c_int), ("causal", C.c_int), ("scale", C.c_float),
                 ("ld_q", C.c_int), ("ld_k", C.c_int), ("ld_v", C.c_int), ("ld_ctx", C.c_int)]
 
     def __init__(self, tokens, sequences, starts, heads, kv_heads, head_dim, causal, scale=0.0, ld_q=0, ld_k=0, ld_v=0,
                  ld_ctx=0):
-        super().__init__(tokens, sequences, _ptr(starts), heads, kv_heads, head_dim, int(causal), scale, ld_q, ld_k,
-                         ld_v, ld_ctx)
+        super().__init__(tokens, sequences, _kernel_array("starts", starts, "int32", sequences + 1), heads, kv_heads,
+                         head_dim, int(causal), scale, ld_q, ld_k, ld_v, ld_ctx)
         self._starts = starts
 
 
 class bp_relpos(C.Structure):
-    """Relative position bias.  `table`: fp32 device tensor [buckets, heads] (kept alive by this object) or its address."""
+    """Relative position bias.  `table`: contiguous fp32 device tensor [buckets, heads] (kept alive by this object) or its
+    address."""
     _fields_ = [("buckets", C.c_int), ("max_distance", C.c_int), ("table", C.c_void_p)]
 
     def __init__(self, buckets, max_distance, table):
-        super().__init__(buckets, max_distance, _ptr(table))
+        super().__init__(buckets, max_distance, _kernel_array("table", table, "float32", buckets))
         self._table = table
+
+    def _for_heads(self, heads):
+        """This, if its table has a value for each bucket and head."""
+        if not isinstance(self._table, int) and self._table is not None and self._table.numel() < self.buckets * heads:
+            raise BitPipeError(BP_EINVAL, f"table must be [{self.buckets}, {heads}], not {tuple(self._table.shape)}")
+        return self
 
 
 class BitPipeError(RuntimeError):
@@ -440,6 +461,8 @@ def bp_relpos_bucket(causal, buckets, max_distance, offset) -> int:
 
 
 def bp_op_attention_packed_fwd(dtype, layout, q, k, v, ctx, lse, bias=None, stream=None):
+    if bias is not None and layout is not None:
+        bias._for_heads(layout.heads)
     return _check(lib().bp_op_attention_packed_fwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
                                                    stream))
 
@@ -450,8 +473,13 @@ def bp_op_attention_packed_workspace(dtype, layout, bias=None) -> int:
 
 def bp_op_attention_packed_bwd(dtype, layout, q, k, v, ctx, lse, dctx, dq, dk, dv, workspace, bias=None, dtable=None,
                                overwrite=0, workspace_elems=None, stream=None):
-    """workspace_elems: fp32 elements of the workspace (default: those of the tensor)."""
-    n = workspace_elems if workspace_elems is not None else workspace.numel() if workspace is not None else 0
+    """workspace_elems: fp32 elements of the workspace (default: what the tensor has room for)."""
+    n = workspace_elems
+    if n is None:
+        n = workspace.numel() * workspace.element_size() // 4 if workspace is not None else 0
+    if bias is not None and layout is not None:
+        bias._for_heads(layout.heads)
+        dtable = _kernel_array("dtable", dtable, "float32", bias.buckets * layout.heads)
     return _check(lib().bp_op_attention_packed_bwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
                                                    _ptr(dctx), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), overwrite,
                                                    _ptr(workspace), n, stream))
