@@ -408,7 +408,7 @@ int bp_op_attention_bwd(int dtype, int B, int S, int heads, int head_dim, int ca
  * earlier tokens under a causal mask, keep their results.  Results must not overlap inputs or each other. */
 typedef struct {
     int tokens;             /* rows of every tensor, below 2^24; (tokens + 63) / 64 * heads, too     */
-    int sequences;          /* >= 1                                                                  */
+    int sequences;          /* >= 1, below 2^24                                                      */
     const int32_t* starts;  /* dev [sequences + 1], ascending, within 0 .. tokens                    */
     int heads, kv_heads;    /* heads a multiple of kv_heads                                          */
     int head_dim;           /* 1 .. 512; matrix-core kernels: multiples of 8 up to 128, rows and     */

@@ -70,6 +70,8 @@ int make_args(int dtype, const bp_packed* p, const bp_relpos* bias, PackedArgs& 
         return fail(BP_EINVAL, "tokens, sequences, heads, kv_heads, head_dim must be positive");
     if (p->heads % p->kv_heads) return fail(BP_EINVAL, "%d heads cannot share %d key/value heads evenly", p->heads, p->kv_heads);
     if (!(p->scale >= 0.f) || isinf(p->scale)) return fail(BP_EINVAL, "scale must be positive and finite, or 0");
+    // (the kernels count starts in 32 bits, and one wave may have to look at all that share a row)
+    if (p->sequences >= 1 << 24) return fail(BP_ESHAPE, "sequences = %d must be below 2^24", p->sequences);
     if (p->tokens >= 1 << 24) return fail(BP_ESHAPE, "tokens = %d must be below 2^24", p->tokens);
     if (p->head_dim > kPackedMaxHeadDim) return fail(BP_ESHAPE, "head_dim = %d must be at most %d", p->head_dim, kPackedMaxHeadDim);
     if (p->heads > 65535 / 8) return fail(BP_ESHAPE, "heads = %d must be at most %d", p->heads, 65535 / 8);

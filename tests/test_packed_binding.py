@@ -76,3 +76,15 @@ def test_what_is_right_is_taken():
     layout, bias = bp.bp_packed(starts=starts, **LAYOUT), bp.bp_relpos(32, 128, table)
     assert layout.starts == starts.data_ptr() and bias.table == table.data_ptr()
     assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout, bias) > 0
+
+
+@pytest.mark.parametrize("sequences", [1 << 24, (1 << 31) - 64, (1 << 31) - 1])
+def test_more_sequences_than_tokens_can_be_refused(sequences):
+    layout = bp.bp_packed(starts=4096, **{**LAYOUT, "sequences": sequences})
+    assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, layout) == 0
+    for call in (lambda: bp.bp_op_attention_packed_fwd(bp.BP_BF16, layout, *ADDRESSES),
+                 lambda: bp.bp_op_attention_packed_bwd(bp.BP_BF16, layout, *ADDRESSES, *[4096] * 4, 4096, workspace_elems=1 << 30)):
+        with pytest.raises(bp.BitPipeError) as e:
+            call()
+        assert e.value.code == bp.BP_ESHAPE
+    assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, bp.bp_packed(starts=4096, **{**LAYOUT, "sequences": (1 << 24) - 1})) > 0
