@@ -87,7 +87,9 @@ int make_args(int dtype, const bp_packed* p, const bp_relpos* bias, PackedArgs& 
         return fail(BP_EINVAL, "leading dimension smaller than the row length");
     if (a.ld_q >= 1 << 24 || a.ld_k >= 1 << 24 || a.ld_v >= 1 << 24 || a.ld_o >= 1 << 24)
         return fail(BP_ESHAPE, "leading dimensions must be below 2^24");
-    // (a launch has fewer than 2^32 threads)
+    // A launch of the kernels of 64 rows has up to this many blocks of 256 threads, and fewer than 2^32 threads: forward and dQ
+    // a block for each tile and head, dK/dV for each tile and part of the heads.  (One row a block: tokens below 2^24 keep the
+    // grid's first dimension there, heads are its second; the joined sums' launch: see launch_dkv.)
     if ((int64_t)packed_tiles(a.T) * a.heads >= 1 << 24)
         return fail(BP_ESHAPE, "%d tokens of %d heads: (tokens + 63) / 64 * heads must be below 2^24", a.T, a.heads);
     if (bias) {
