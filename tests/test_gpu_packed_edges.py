@@ -1,5 +1,5 @@
 """GPU: attention over packed sequences where a row holds what is not finite or sees nothing, where a bucket of the bias is far
-from every score, against a 64-bit form that takes visible pairs only; and the precision of the kernels of one row a block."""
+from every score, against a 64-bit form that takes visible pairs only; the precision of the kernels of one row a block; and sequences of thousands of tokens."""
 import numpy as np
 import pytest
 
@@ -163,3 +163,82 @@ def test_row_kernels_long_sums():
         bound = r["abs_" + name] * (share + (t + 2 * d + 64) * f)
         off = np.max(np.abs(got[name] - r[name]) / (bound + 1e-30))
         assert off <= 1.0, (name, float(off))
+
+
+def in_64_bits(c):
+    """po.attention's dict from whole matrices in fp64 on the GPU, a head at a time (finite inputs).  A value of the table beyond
+    1e6 takes no part in "z": pairs that have it have no probability."""
+    import torch
+    dev = dict(dtype=torch.float64, device="cuda")
+    q, k, v, g = (torch.tensor(x, **dev) for x in (c.q, c.k, c.v, c.g))
+    G = c.H // c.Hk
+    r = {n: torch.zeros(s, **dev) for n, s in (("ctx", c.q.shape), ("lse", (c.H, c.T)), ("dq", c.q.shape), ("dk", c.k.shape), ("dv", c.v.shape))}
+    r |= {"abs_" + n: torch.zeros_like(t) for n, t in r.items()}
+    if c.table is not None:
+        table = torch.tensor(c.table, **dev)
+        size = torch.where(table.abs() < 1e6, table.abs(), 0.0)
+        r |= {"dtable": torch.zeros_like(table), "abs_dtable": torch.zeros_like(table)}
+    z_most = 0.0
+    for s0, s1 in zip(c.starts[:-1], c.starts[1:]):
+        n, R = s1 - s0, slice(s0, s1)
+        if not n:
+            continue
+        at = torch.arange(n, device="cuda")
+        offset = at[None] - at[:, None]
+        later = offset > 0
+        if c.table is not None:
+            by_offset = torch.tensor([po.bucket(c.causal, len(c.table), c.far, o) if not (c.causal and o > 0) else 0
+                                      for o in range(1 - n, n)], device="cuda")
+            of = by_offset[offset + n - 1]
+        for h in range(c.H):
+            Q, K, V, D = q[R, h], k[R, h // G], v[R, h // G], g[R, h]
+            z, zabs = c.scale * (Q @ K.t()), c.scale * (Q.abs() @ K.abs().t())
+            if c.table is not None:
+                z, zabs = z + table[:, h][of], zabs + size[:, h][of]
+            if c.causal:
+                z, zabs = z.masked_fill(later, -float("inf")), zabs.masked_fill(later, 0.0)
+            z_most = max(z_most, float(zabs.max()))
+            r["lse"][h, R] = torch.logsumexp(z, 1)
+            p = torch.softmax(z, 1)
+            dp, dpa = D @ V.t(), D.abs() @ V.abs().t()
+            ds = p * (dp - (p * dp).sum(1, keepdim=True))
+            dsa = p * (dpa + (p * dpa).sum(1, keepdim=True))
+            r["ctx"][R, h], r["abs_ctx"][R, h] = p @ V, p @ V.abs()
+            r["dq"][R, h], r["abs_dq"][R, h] = c.scale * (ds @ K), c.scale * (dsa @ K.abs())
+            r["dk"][R, h // G] += c.scale * (ds.t() @ Q)
+            r["abs_dk"][R, h // G] += c.scale * (dsa.t() @ Q.abs())
+            r["dv"][R, h // G] += p.t() @ D
+            r["abs_dv"][R, h // G] += p.t() @ D.abs()
+            if c.table is not None:
+                for name, x in (("dtable", ds), ("abs_dtable", dsa)):       # along the diagonals first: each row moved on by one
+                    x = torch.nn.functional.pad(x.flip(0), (0, n)).flatten()[:-n].view(n, 2 * n - 1).sum(0)
+                    r[name][:, h].index_add_(0, by_offset, x)
+    r["abs_lse"] = r["lse"].abs()
+    return {n: t.cpu().numpy() for n, t in r.items()} | {"z": z_most}
+
+
+# Sequences of thousands of tokens: far pieces of one bucket, borders of buckets far from the diagonal, hundreds of steps;
+# few blocks, blocks of two heads, of 128 rows
+@pytest.mark.parametrize("lens,H,Hk,d,causal", [([2900, 37, 1200], 4, 2, 128, True), ([5091], 2, 1, 64, False), ([17, 4100], 32, 8, 64, True),
+                                                ([2500, 2500], 16, 16, 128, True)])
+@pytest.mark.parametrize("buckets,far", [(0, 0), (32, 128), (64, 3000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_long_sequences(dtype, buckets, far, lens, H, Hk, d, causal):
+    if dtype == "f32":
+        H, Hk = H // Hk, 1
+    c = Call(lens, H, Hk, d, causal, dtype, front=1, back=6, buckets=buckets, far=far, fused=True)
+    c.check(c.run(), in_64_bits(c))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_row_kernels_long_sequences(dtype):
+    c = Call([1700, 33], 2, 1, 20, True, dtype, front=1, back=2, buckets=32, far=500, shift=1)
+    c.check(c.run(), in_64_bits(c))
+
+
+@pytest.mark.parametrize("H,Hk,d", [(32, 8, 64), (33, 11, 64), (16, 8, 128)])
+def test_bucket_far_from_all_scores_in_wide_blocks(H, Hk, d):
+    """The same in launches of blocks of two heads and of 128 rows."""
+    c = Call([2100, 70, 2000], H, Hk, d, True, "bf16", back=2, buckets=16, far=40, std=8.0)
+    c.table[15] = -1e12
+    c.check(c.run(), in_64_bits(c))
