@@ -743,7 +743,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 __syncthreads();
                 sum = ex[(wave & 2) * 64 + lane] + ex[(wave | 1) * 64 + lane];
             }
-            if (all || (x.lo >= x.short_lo && x.hi <= x.short_hi)) delta = sum;        // all of the row's keys were there
+            if (all || x.hi - x.lo <= kShort) delta = sum;          // (a rule on the row alone, whatever else was walked)
             __syncthreads();                // (and the stages are free for the next walk)
         } else if (grad) {
             flush();

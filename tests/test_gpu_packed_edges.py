@@ -242,3 +242,27 @@ def test_bucket_far_from_all_scores_in_wide_blocks(H, Hk, d):
     c = Call([2100, 70, 2000], H, Hk, d, True, "bf16", back=2, buckets=16, far=40, std=8.0)
     c.table[15] = -1e12
     c.check(c.run(), in_64_bits(c))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradient_of_a_row_does_not_depend_on_what_lies_behind_it(d, causal):
+    """How delta of a bf16 row is found depends on its own number of keys: with the forward's results given, dQ of a sequence
+    has the same bits with and without a short sequence behind it in its last block, which holds rows of 217 to 270 keys."""
+    import torch
+    import paper_2410_19367_amd as bp
+    H, Hk, front, n, more = 4, 2, 40, 270, 10
+    c = Call([n, more], H, Hk, d, causal, "bf16", front=front)
+    end = front + n
+    q, k, v, g = (torch.tensor(x.reshape(end + more, -1), dtype=torch.bfloat16, device="cuda") for x in (c.q, c.k, c.v, c.g))
+    ctx, lse, seen = torch.zeros_like(q), torch.zeros((H, end + more), device="cuda"), []
+    bp.bp_op_attention_packed_fwd(c.dt, bp.bp_packed(end + more, 2, c.starts_dev, H, Hk, d, causal), q, k, v, ctx, lse)
+    for sequences, T in ((2, end + more), (1, end + more), (1, end)):       # the short sequence, rows of none, nothing
+        layout = bp.bp_packed(T, sequences, c.starts_dev, H, Hk, d, causal)
+        a = [t[:T] for t in (q, k, v, ctx)]
+        dq, dk, dv = (torch.zeros_like(t) for t in a[:3])
+        ws = torch.zeros(bp.bp_op_attention_packed_workspace(c.dt, layout), device="cuda")
+        bp.bp_op_attention_packed_bwd(c.dt, layout, *a, lse[:, :T].contiguous(), g[:T], dq, dk, dv, ws)
+        seen.append(dq[front:end])
+    torch.cuda.synchronize()
+    assert torch.equal(seen[0], seen[1]) and torch.equal(seen[0], seen[2])
