@@ -454,10 +454,13 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
             if (masked) {
                 asm volatile("");           // keeps the condition a branch, not a select per pair of every tile
 #pragma unroll
-                for (int u = 0; u < NH; ++u)
+                for (int u = 0; u < NH; ++u) {
+                    // (a row that sees nothing of the piece: its bucket's bias may be NaN or infinite)
+                    if (BIAS && (kw + 32 * u >= x.hi || kw + 32 * u + 32 <= x.lo)) o[u] = 0.f;
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
                         if ((unsigned)(kw + 32 * u + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) s[u][v] = -INFINITY;
+                }
             }
             float mx = -INFINITY, w[NH];
 #pragma unroll
@@ -698,6 +701,7 @@ __global__ __launch_bounds__(256, P::D * sizeof(typename P::elem) <= 256 ? 2 : 1
                 const bool masked = kw < x.inner_lo || kw + 32 > x.inner_hi;
                 if (masked) {
                     asm volatile("");
+                    if (BIAS && walk == DELTA && (kw >= x.hi || kw + 32 <= x.lo)) o = -lse;     // (as in the forward)
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
                         if ((unsigned)(kw + piece_row(v, h) - x.lo) >= (unsigned)(x.hi - x.lo)) {

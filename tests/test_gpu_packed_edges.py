@@ -266,3 +266,17 @@ def test_gradient_of_a_row_does_not_depend_on_what_lies_behind_it(d, causal):
         seen.append(dq[front:end])
     torch.cuda.synchronize()
     assert torch.equal(seen[0], seen[1]) and torch.equal(seen[0], seen[2])
+
+
+@pytest.mark.parametrize("d,shift", KERNELS)
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("lens,causal", [([100, 30], True), ([20, 100, 17], False), ([300, 20, 60], True), ([20, 300], False)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bucket_that_is_not_finite_reaches_queries_that_see_it(dtype, lens, causal, value, d, shift):
+    """Sequences too short for the far bucket keep their results, also where they share a block with one that has it."""
+    c = Call(lens, 4, 2, d, causal, dtype, front=3, back=5, buckets=16, far=40, shift=shift)
+    c.table[[15] if causal else [7, 15], 1] = value
+    r = by_rows(c)
+    assert np.isnan(r["ctx"][:, 1]).any() and np.isfinite(r["ctx"][:, [0, 2, 3]]).all()
+    assert any(np.isfinite(r["dq"][s0:s1]).all() for s0, s1 in zip(c.starts[:-1], c.starts[1:]))
+    check(c, c.run(), r)
