@@ -405,7 +405,8 @@ int bp_op_attention_bwd(int dtype, int B, int S, int heads, int head_dim, int ca
  * Row t, head h, element c of a tensor lies at t * ld + h * head_dim + c; gradients lie as the tensors they belong to
  * (dq as q, dk as k, dv as v, dctx as ctx).  bf16 products take the probabilities and the score gradients rounded to
  * bf16; sums and softmax are fp32.  A value that is not finite reaches only what depends on it: other sequences, and
- * earlier tokens under a causal mask, keep their results.  Results must not overlap inputs or each other. */
+ * earlier tokens under a causal mask, keep their results (in bf16 within these roundings: rows that share a block of 64 or
+ * 128 with NaN get theirs from unrounded probabilities).  Results must not overlap inputs or each other. */
 typedef struct {
     int tokens;             /* rows of every tensor, below 2^24; (tokens + 63) / 64 * heads, too     */
     int sequences;          /* >= 1, below 2^24                                                      */
@@ -444,7 +445,8 @@ size_t bp_op_attention_packed_workspace(int dtype, const bp_packed* layout, cons
 
 /* dq, dk and dv from dctx and the forward's inputs, ctx and lse.  dtable: dev fp32 [buckets, heads], receives += the
  * gradient of the bias table, overwrite != 0: = (NULL: not wanted; with bf16 it costs a second look at the keys, since the
- * rounding of ctx would be felt in it).  workspace: dev fp32, aligned to 16 bytes; its contents need no clearing, and calls that run at the same
+ * rounding of ctx would be felt in it, and dq and dk, too, are then free of that rounding, as rows of up to 256 keys always
+ * are).  workspace: dev fp32, aligned to 16 bytes; its contents need no clearing, and calls that run at the same
  * time need one each.  The result does not depend on anything but the arguments: no atomic adds across blocks. */
 int bp_op_attention_packed_bwd(int dtype, const bp_packed* layout, const bp_relpos* bias, const void* q,
                                const void* k, const void* v, const void* ctx, const float* lse, const void* dctx,

@@ -51,6 +51,11 @@ struct PackedArgs {
 // memory, which long sequences pay and short ones do not.  Whole backward with 1 / 2 / 4 blocks a CU, us, from 256 of one
 // part on: one sequence of 8192, 8 heads of 128 on 2 905 / 624 / 508; 2048 tokens, 32 on 8 252 / 187 / 168; 4 sequences
 // of 512 92.7 / 89.3 / 96.8; from 512, 16 of 256 tokens 100 / 99 / 125; 200 of 1 to 40, 32 of 96 on 4 73 / 81 / 92.
+// The host does not know the lengths, so the rule goes by their mean, empty sequences and rows of none included.  Where they
+// differ: 3000, 517, 1777, 90 and 408 tokens, 8 heads of 128 on 2 215 / 161 / 162, 16 on 4 376 / 273 / 266; 2000, 30, 500,
+// 10, 1, 700, 32 of 128 on 8 274 / 211 / 228: the second of each, as it should be.  One long sequence among many short or
+// empty ones is taken for short: 4000 and 200 of 20, 32 of 96 on 4 716 / 501 / 446; 4096 and 60 empty, 8 of 128 on 2
+// 257 / 185 / 186; 1500 and 20 of 20, 32 of 64 on 4 80 / 71 / 71: the first of each, up to 1.6 times the best.
 inline int split_heads(const PackedArgs& a, int cus) {
     const int G = a.heads / a.kv_heads, mean = a.T / a.n_seq, blocks = mean >= 1024 ? 4 : mean >= 128 ? 2 : 1;
     const long one = (long)((a.T + kPackedTile - 1) / kPackedTile) * a.kv_heads;

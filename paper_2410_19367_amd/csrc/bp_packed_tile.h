@@ -250,7 +250,7 @@ __device__ __forceinline__ void wave_sync() {
 // Sums of a piece along its offsets: lane o < 63 gets the sum over the rows r of what lane r - o + 31 of a half has for row r.
 // Eight rows at a time go to LDS, each moved on by its place, and come back as columns: 16 writes and 32 reads without a
 // bank conflict.  (16 ds_add_f32 at the offsets, some 2.5 cycles a lane each: dQ with the table's gradient, 8 sentences, 16
-// heads of 64, 130 us, now 67; 6 documents, 32 heads of 128, 1160 us, now 615.)  What the writes leave out is zero throughout.
+// heads of 64, 130 us, now 68; 6 documents, 32 heads of 128, 1160 us, now 608.)  What the writes leave out is zero throughout.
 constexpr int kSkewPitch = 40;              // offsets 0 .. 38 of eight rows, and a column of zeros
 __device__ __forceinline__ float sum_by_offset(float* skew, const f32x16& x, int lane) {
     const int h = lane >> 5;

@@ -85,11 +85,12 @@ KERNELS = [(64, 0), (128, 0), (64, 1)]
 @pytest.mark.parametrize("lens,causal,at", [([40, 24], True, 50), ([24, 40], True, 20), ([300, 3], True, 301), ([2, 300, 60], True, 30),
                                             ([40, 24], False, 50), ([300, 3], False, 301)])
 @pytest.mark.parametrize("where", ["q", "g", "k", "v"])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_table_gradient_takes_nothing_from_pairs_that_are_not_visible(dtype, where, lens, causal, at, d, shift):
-    """NaN in a row inside a sequence reaches the buckets of the distances that its queries see, in its heads, and no others."""
+def test_table_gradient_takes_nothing_from_pairs_that_are_not_visible(dtype, value, where, lens, causal, at, d, shift):
+    """NaN or infinity in a row inside a sequence reaches the buckets of the distances that its queries see, in its heads, and no others."""
     c = Call(lens, 4, 2, d, causal, dtype, front=3, back=5, buckets=16, far=40, shift=shift)
-    getattr(c, where)[c.starts[0] + at, 1, 3] = np.nan
+    getattr(c, where)[c.starts[0] + at, 1, 3] = value
     for x in (c.q, c.k, c.v, c.g):
         x[:3] = np.nan
         x[c.starts[-1]:] = np.nan
