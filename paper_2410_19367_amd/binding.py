@@ -88,12 +88,6 @@ class bp_relpos(C.Structure):
         super().__init__(buckets, max_distance, _kernel_array("table", table, "float32", buckets))
         self._table = table
 
-    def _for_heads(self, heads):
-        """This, if its table has a value for each bucket and head."""
-        if not isinstance(self._table, int) and self._table is not None and self._table.numel() < self.buckets * heads:
-            raise BitPipeError(BP_EINVAL, f"table must be [{self.buckets}, {heads}], not {tuple(self._table.shape)}")
-        return self
-
 
 class BitPipeError(RuntimeError):
     def __init__(self, code, msg):
@@ -460,9 +454,15 @@ def bp_relpos_bucket(causal, buckets, max_distance, offset) -> int:
     return b
 
 
+def _check_table(layout, bias):
+    """The bias table has a value for each bucket and head, where both are objects of this module."""
+    table = getattr(bias, "_table", None)
+    if hasattr(table, "numel") and isinstance(layout, bp_packed) and table.numel() < bias.buckets * layout.heads:
+        raise BitPipeError(BP_EINVAL, f"table must be [{bias.buckets}, {layout.heads}], not {tuple(table.shape)}")
+
+
 def bp_op_attention_packed_fwd(dtype, layout, q, k, v, ctx, lse, bias=None, stream=None):
-    if bias is not None and layout is not None:
-        bias._for_heads(layout.heads)
+    _check_table(layout, bias)
     return _check(lib().bp_op_attention_packed_fwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
                                                    stream))
 
@@ -477,8 +477,8 @@ def bp_op_attention_packed_bwd(dtype, layout, q, k, v, ctx, lse, dctx, dq, dk, d
     n = workspace_elems
     if n is None:
         n = workspace.numel() * workspace.element_size() // 4 if workspace is not None else 0
-    if bias is not None and layout is not None:
-        bias._for_heads(layout.heads)
+    _check_table(layout, bias)
+    if isinstance(bias, bp_relpos) and isinstance(layout, bp_packed):
         dtable = _kernel_array("dtable", dtable, "float32", bias.buckets * layout.heads)
     return _check(lib().bp_op_attention_packed_bwd(dtype, layout, bias, _ptr(q), _ptr(k), _ptr(v), _ptr(ctx), _ptr(lse),
                                                    _ptr(dctx), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), overwrite,

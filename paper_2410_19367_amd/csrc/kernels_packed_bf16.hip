@@ -1,5 +1,6 @@
 // Attention over packed sequences, bf16: the kernels of bp_packed_tile.h on v_mfma_f32_32x32x16_bf16.  P and dS are rounded
-// to bf16 for the second products (half a step of 2^-8 of each term, below the rounding of the results); scores, softmax,
+// to bf16 for the second products, 2^-8 of each term at most; what that leaves in a result is about as large as the rounding
+// of the result itself (forward and backward off by 2.4e-3 of the exact results, these rounded by 1.7e-3).  Scores, softmax,
 // sums and the table's gradient are fp32.
 #include "bp_attn_bf16.h"
 #include "bp_packed_tile.h"

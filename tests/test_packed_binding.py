@@ -88,3 +88,13 @@ def test_more_sequences_than_tokens_can_be_refused(sequences):
             call()
         assert e.value.code == bp.BP_ESHAPE
     assert bp.bp_op_attention_packed_workspace(bp.BP_BF16, bp.bp_packed(starts=4096, **{**LAYOUT, "sequences": (1 << 24) - 1})) > 0
+
+
+def test_pointers_to_the_structures_are_taken():
+    """As ctypes takes them: refused for what they point at only."""
+    import ctypes as C
+    layout, bias = bp.bp_packed(starts=4096, **LAYOUT), bp.bp_relpos(32, 3, 4096)
+    for b in (C.byref(bias), C.pointer(bias), bias):
+        refused(lambda: bp.bp_op_attention_packed_fwd(bp.BP_BF16, C.byref(layout), *ADDRESSES, bias=b), "max_distance")
+        refused(lambda: bp.bp_op_attention_packed_bwd(bp.BP_BF16, C.byref(layout), *ADDRESSES, *[4096] * 4, 4096, bias=b, dtable=4096,
+                                                      workspace_elems=1 << 30), "max_distance")
