@@ -1062,7 +1062,7 @@ static hipError_t launch_dkv(const PackedArgs& a, hipStream_t s) {
     const hipError_t e = allow_lds(packed_dkv_kernel<P, BIAS>, smem, set);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((packed_dkv_kernel<P, BIAS>), dim3(packed_tiles(a.T) * a.kv_heads * a.splits), dim3(256), smem, s, a);
-    // (parts are for launches of fewer than 4 blocks a CU, so rows * kv_heads stays below 256 CUs' 65536 and threads below 2^23)
+    // (parts are for launches of fewer than 4 blocks a CU, so rows * kv_heads stays below 65536 on 256 CUs, threads below 2^23)
     const size_t threads = a.splits > 1 ? (size_t)a.T * (a.kv_heads * 2 * a.d / 4) : 0;
     const unsigned blocks = (unsigned)((threads + 255) / 256) + (a.table_part ? a.heads : 0);
     if (blocks) hipLaunchKernelGGL((packed_join_kernel<P>), dim3(blocks), dim3(256), 0, s, a);
